@@ -35,6 +35,11 @@ EXPORTS = ("np_status_str", "np_last_error", "np_shape_check", "np_workspace_siz
            "np_percentile", "np_threshold_active", "np_stage_file", "np_read_records",
            "np_device_error", "np_sparse_mlp_noalloc", "np_sparse_mlp_ids", "np_select_delta")
 
+# every symbol neuroprefetch_kv.h declares
+KV_EXPORTS = ("np_kv_shape_check", "np_kv_workspace_size", "np_kv_reset", "np_kv_extend",
+              "np_kv_fork", "np_kv_free", "np_kv_compact", "np_kv_append", "np_attn_decode",
+              "np_attn_prompt")
+
 
 class NPError(RuntimeError):
     def __init__(self, status: int, fn: str, detail: str):
@@ -67,6 +72,34 @@ class np_centroid_model(ctypes.Structure):
 class np_stage_plan(ctypes.Structure):
     _fields_ = [("counts", ctypes.c_void_p), ("in_ids", ctypes.c_void_p),
                 ("in_slots", ctypes.c_void_p)]
+
+
+# the paged key-value cache and its attention (neuroprefetch_kv.h)
+class np_kv_shape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("layers", "heads", "kv_heads", "head_dim", "page_size", "n_pages", "max_seqs",
+                 "seq_pages", "dtype")]
+
+
+class np_kv_state(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("page_table", "kv_len", "refs")]
+
+
+class np_kv_batch(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int32), ("n_tokens", ctypes.c_int32),
+                ("max_tokens", ctypes.c_int32), ("max_len", ctypes.c_int32),
+                ("seqs", ctypes.c_void_p), ("cu_tokens", ctypes.c_void_p),
+                ("pos0", ctypes.c_void_p)]
+
+
+class np_kv_rows(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("q", "k", "v", "q_out")] +
+                [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride")])
+
+
+class np_rotary(ctypes.Structure):
+    _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("dim", ctypes.c_int32),
+                ("max_pos", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
 
 
 _lib = None
@@ -116,7 +149,21 @@ def lib():
         L.np_stage_file.argtypes = [S, ctypes.POINTER(np_stage_plan), i32, i32, i32, i64, vp, vp,
                                     sz, vp, sz, vp, sz, vp, vp, vp]
         L.np_read_records.argtypes = [i32, i64, i64, vp, i32, vp]
-        for f in EXPORTS[2:]:
+        K = ctypes.POINTER(np_kv_shape)
+        KS, KB = ctypes.POINTER(np_kv_state), ctypes.POINTER(np_kv_batch)
+        L.np_kv_shape_check.argtypes = [K]
+        L.np_kv_workspace_size.argtypes = [K, ctypes.POINTER(sz)]
+        L.np_kv_reset.argtypes = [K, KS, vp, vp]
+        L.np_kv_extend.argtypes = [K, KS, vp, i32, vp, vp, vp, vp, vp]
+        L.np_kv_fork.argtypes = [K, KS, i32, vp, vp, vp, vp, vp]
+        L.np_kv_free.argtypes = [K, KS, i32, vp, vp, vp]
+        L.np_kv_compact.argtypes = [K, KS, vp, vp, vp, vp]
+        L.np_kv_append.argtypes = [K, i32, KB, vp, ctypes.POINTER(np_kv_rows),
+                                   ctypes.POINTER(np_rotary), vp, vp, vp]
+        L.np_attn_decode.argtypes = [K, i32, KB, vp, vp, i64, vp, ctypes.c_float, i32, vp, i64, vp,
+                                     vp]
+        L.np_attn_prompt.argtypes = L.np_attn_decode.argtypes
+        for f in EXPORTS[2:] + KV_EXPORTS:
             getattr(L, f).restype = i32
         _lib = L
     return _lib
@@ -338,6 +385,114 @@ def np_device_error(ws, stream=None) -> int:
     code = ctypes.c_int32(0)
     _check(lib().np_device_error(_p(ws), _s(stream), ctypes.byref(code)), "np_device_error")
     return code.value
+
+
+# ---------------------------------------------------------------------------
+# the paged key-value cache and its attention
+# ---------------------------------------------------------------------------
+
+def _kept(s: ctypes.Structure, *tensors):
+    """The structure, keeping the tensors it points into alive."""
+    s._kept = tensors
+    return s
+
+
+def make_kv_shape(layers, heads, kv_heads, head_dim, page_size, n_pages, max_seqs, seq_pages,
+                  dtype) -> np_kv_shape:
+    return np_kv_shape(layers, heads, kv_heads, head_dim, page_size, n_pages, max_seqs, seq_pages,
+                       DTYPE_CODE.get(dtype, dtype))
+
+
+def make_kv_state(page_table, kv_len, refs) -> np_kv_state:
+    return _kept(np_kv_state(_p(page_table), _p(kv_len), _p(refs)), page_table, kv_len, refs)
+
+
+def make_kv_batch(n_seq: int, n_tokens: int, max_tokens: int, max_len: int, pos0, seqs=None,
+                  cu_tokens=None) -> np_kv_batch:
+    return _kept(np_kv_batch(n_seq, n_tokens, max_tokens, max_len, _p(seqs), _p(cu_tokens),
+                             _p(pos0)), pos0, seqs, cu_tokens)
+
+
+def _token_stride(x) -> int:
+    """Token stride, in elements, of a [tokens][heads][head_dim] tensor (heads contiguous)."""
+    if x.dim() != 3 or x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2]):
+        raise ValueError("need a [tokens][heads][head_dim] tensor whose heads are contiguous")
+    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0), x.shape[1] * x.shape[2])
+
+
+def make_qkv(q, k, v, q_out) -> np_kv_rows:
+    """np_kv_rows of [tokens][heads][head_dim] tensors (views of one projection, say)."""
+    t = (q, k, v, q_out)
+    return _kept(np_kv_rows(*[_p(x) for x in t], *[_token_stride(x) for x in t]), *t)
+
+
+def make_rotary(cos, sin, interleaved: bool = False) -> np_rotary:
+    """cos and sin: float32 [max_pos][dim / 2], contiguous."""
+    if cos.shape != sin.shape or not (cos.is_contiguous() and sin.is_contiguous()):
+        raise ValueError("cos and sin: contiguous [max_pos][dim / 2] tensors of one shape")
+    return _kept(np_rotary(_p(cos), _p(sin), 2 * cos.shape[1], cos.shape[0], int(interleaved)),
+                 cos, sin)
+
+
+def np_kv_shape_check(shape: np_kv_shape) -> None:
+    _check(lib().np_kv_shape_check(ctypes.byref(shape)), "np_kv_shape_check")
+
+
+def np_kv_workspace_size(shape: np_kv_shape) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().np_kv_workspace_size(ctypes.byref(shape), ctypes.byref(n)), "np_kv_workspace_size")
+    return n.value
+
+
+def np_kv_reset(shape, state: np_kv_state, ws, stream=None) -> None:
+    _check(lib().np_kv_reset(ctypes.byref(shape), ctypes.byref(state), _p(ws), _s(stream)),
+           "np_kv_reset")
+
+
+def np_kv_extend(shape, state: np_kv_state, pool, n_seq: int, seqs, n_new, pos0, ws,
+                 stream=None) -> None:
+    _check(lib().np_kv_extend(ctypes.byref(shape), ctypes.byref(state), _p(pool), int(n_seq),
+                              _p(seqs), _p(n_new), _p(pos0), _p(ws), _s(stream)), "np_kv_extend")
+
+
+def np_kv_fork(shape, state: np_kv_state, n: int, src, dst, lens, ws, stream=None) -> None:
+    _check(lib().np_kv_fork(ctypes.byref(shape), ctypes.byref(state), int(n), _p(src), _p(dst),
+                            _p(lens), _p(ws), _s(stream)), "np_kv_fork")
+
+
+def np_kv_free(shape, state: np_kv_state, n: int, seqs, ws, stream=None) -> None:
+    _check(lib().np_kv_free(ctypes.byref(shape), ctypes.byref(state), int(n), _p(seqs), _p(ws),
+                            _s(stream)), "np_kv_free")
+
+
+def np_kv_compact(shape, state: np_kv_state, pool, n_moved, ws, stream=None) -> None:
+    _check(lib().np_kv_compact(ctypes.byref(shape), ctypes.byref(state), _p(pool), _p(n_moved),
+                               _p(ws), _s(stream)), "np_kv_compact")
+
+
+def np_kv_append(shape, layer: int, batch: np_kv_batch, page_table, rows: np_kv_rows, rotary, pool,
+                 ws, stream=None) -> None:
+    _check(lib().np_kv_append(ctypes.byref(shape), int(layer), ctypes.byref(batch), _p(page_table),
+                              ctypes.byref(rows), None if rotary is None else ctypes.byref(rotary),
+                              _p(pool), _p(ws), _s(stream)), "np_kv_append")
+
+
+def np_attn_decode(shape, layer: int, batch: np_kv_batch, page_table, q, pool, scale: float,
+                   window: int, out, ws, stream=None) -> None:
+    """q and out: [tokens][heads][head_dim] tensors."""
+    _check(lib().np_attn_decode(ctypes.byref(shape), int(layer), ctypes.byref(batch),
+                                _p(page_table), _p(q), _token_stride(q), _p(pool), float(scale),
+                                int(window), _p(out), _token_stride(out), _p(ws), _s(stream)),
+           "np_attn_decode")
+
+
+def np_attn_prompt(shape, layer: int, batch: np_kv_batch, page_table, q, pool, scale: float,
+                   window: int, out, ws, stream=None) -> None:
+    """q and out: [tokens][heads][head_dim] tensors."""
+    _check(lib().np_attn_prompt(ctypes.byref(shape), int(layer), ctypes.byref(batch),
+                                _p(page_table), _p(q), _token_stride(q), _p(pool), float(scale),
+                                int(window), _p(out), _token_stride(out), _p(ws), _s(stream)),
+           "np_attn_prompt")
 
 
 def _ev(e) -> int | None:

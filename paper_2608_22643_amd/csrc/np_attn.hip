@@ -48,7 +48,9 @@ struct Tile {
 };
 
 // Block `tile` of the batch; false past the last one.  Every lane of the wave
-// takes part and gets the same result.
+// takes part and gets the same result.  err: where this workgroup reports what
+// is wrong with its row, or nullptr; the one with tile 0 reports every row of a
+// bad cu_tokens (a row without tokens has no block).
 template <int RB>
 __device__ inline bool find_tile(const KvBatch& b, int G, int tile, int32_t* err, Tile* t) {
   int row, blk;
@@ -58,8 +60,12 @@ __device__ inline bool find_tile(const KvBatch& b, int G, int tile, int32_t* err
     blk = tile - row * per;
     if (row >= b.n_seq) return false;
   } else {
-    // blocks of the rows before: a running count, 64 rows at a time
     const int lane = threadIdx.x % WAVE;
+    if (err && tile == 0 && threadIdx.x < WAVE)
+      for (int i = lane; i < b.n_seq; i += WAVE)
+        if (b.cu[i] < 0 || b.cu[i + 1] < b.cu[i] || b.cu[i + 1] > b.n_tokens)
+          atomicOr(err, NP_DEVERR_STATE);
+    // blocks of the rows before: a running count, 64 rows at a time
     int before = 0;
     row = -1;
     for (int base = 0; base < b.n_seq; base += WAVE) {
@@ -82,7 +88,7 @@ __device__ inline bool find_tile(const KvBatch& b, int G, int tile, int32_t* err
   }
   row = __builtin_amdgcn_readfirstlane(row);
   blk = __builtin_amdgcn_readfirstlane(blk);
-  t->row = kv_row(b, row, err);
+  t->row = kv_row(b, row, threadIdx.x == 0 ? err : nullptr);
   t->rho0 = blk * RB;
   t->nrow = min(RB, t->row.n * G - t->rho0);
   if (t->nrow <= 0) return false;
@@ -160,7 +166,7 @@ __global__ __launch_bounds__(ROWS_T) void attn_rows_kernel(AttnArgs a) {
   const int id = blockIdx.x;
   const int h = id % a.Hkv, tile = id / a.Hkv % a.tiles, split = id / a.Hkv / a.tiles;
   Tile t;
-  if (!find_tile<RB>(a.b, a.G, tile, split == 0 && h == 0 && threadIdx.x == 0 ? a.err : nullptr, &t))
+  if (!find_tile<RB>(a.b, a.G, tile, split == 0 && h == 0 ? a.err : nullptr, &t))
     return;
 
   const int kbeg = a.window && t.maxpos >= 0 ? max(0, t.minpos - a.window + 1) : 0;
@@ -472,6 +478,262 @@ __global__ __launch_bounds__(ROWS_T) void attn_join_kernel(AttnArgs a) {
     *(float4*)op = make_float4(f[0], f[1], f[2], f[3]);
 }
 
+// ---------------------------------------------------------------------------
+// Tiles: 128 rows against all their keys, for many 16-bit query rows.  Four
+// waves of 32 rows share K and V in steps of KB keys through LDS (double
+// buffered: the next step's rows are on their way from memory to registers
+// while this one is computed).  S^T = K Q^T and O^T = V^T P^T on 32 x 32 x 16
+// tiles, as in the row blocks: a lane owns query l % 32, its accumulator rows
+// 8 a + 4 h + b (h = l / 32) are keys, and the key slots of the second product
+// are numbered such that its P operand is the lane's own scores.  V comes out
+// of LDS transposed (ds_read_tr: four keys of one column per lane).
+//
+// LDS rows are permuted in 16-byte pieces so that neither the row reads of K
+// (32 rows, one piece) nor the transposed reads of V (8 rows, four pieces)
+// meet in a bank.
+// ---------------------------------------------------------------------------
+constexpr int TB = 128;
+constexpr int TILE_T = 256;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+template <class T>
+__device__ inline f32x16 mfma32(uint4 a, uint4 b, f32x16 c) {
+  if constexpr (T::dtype == NP_F16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+template <int DP>
+struct TileCfg {
+  static constexpr int KB = DP == 256 ? 32 : 64;    // keys of a step
+  static constexpr int CPR = DP / 8;                // 16-byte pieces of a row
+  static constexpr int NL = KB * CPR / TILE_T;      // pieces a thread loads
+  static constexpr int RSTEP = TILE_T / CPR;        // rows between them
+  // piece permutations of K and V rows
+  __device__ static inline int kperm(int row, int c) {
+    return c ^ (DP == 64 ? row >> 1 & 7 : row & 15);
+  }
+  __device__ static inline int vperm(int row, int c) {
+    return c ^ (DP == 64 ? (row >> 1 & 1) << 2 | (row >> 2 & 3) : (row & 3) << 2 | (row >> 2 & 3));
+  }
+};
+
+template <class T, int DP>
+__global__ __launch_bounds__(TILE_T) void attn_tile_kernel(AttnArgs a) {
+  using C = TileCfg<DP>;
+  constexpr int KB = C::KB, CPR = C::CPR, NL = C::NL, RSTEP = C::RSTEP;
+  constexpr int KT = KB / 32, KD = DP / 16, DT = DP / 32;
+  __shared__ uint4 s_k[2][KB * CPR];
+  __shared__ uint4 s_v[2][KB * CPR];
+
+  const int tid = threadIdx.x, lane = tid % WAVE;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
+  const int r = lane & 31, h2 = lane >> 5;
+  const int h = blockIdx.x % a.Hkv;
+  const int tile = a.tiles - 1 - (int)blockIdx.x / a.Hkv;  // the longest of a prompt first
+  Tile t;
+  if (!find_tile<TB>(a.b, a.G, tile, h == 0 ? a.err : nullptr, &t)) return;
+
+  const int kbeg = a.window && t.maxpos >= 0 ? max(0, t.minpos - a.window + 1) : 0;
+  const int kend = t.maxpos + 1;
+  const int rowb = a.D * 2;
+
+  // this wave's rows and this lane's query
+  const int w0 = min(wave * 32, t.nrow - 1), w1 = min(wave * 32 + 31, t.nrow - 1);
+  const int wmin = t.row.p0 < 0 ? -1 : t.row.p0 + (t.rho0 + w0) / a.G;
+  const int wmax = t.row.p0 < 0 ? -1 : t.row.p0 + (t.rho0 + w1) / a.G;
+  const int rho = t.rho0 + min(wave * 32 + r, t.nrow - 1);
+  const int tok = rho / a.G, head = h * a.G + rho % a.G;
+  const int qpos = t.row.p0 < 0 ? -1 : t.row.p0 + tok;
+  const char* qp = a.q + (int64_t)(t.row.begin + tok) * a.q_stride + (int64_t)head * rowb;
+  // a negative scale turns into negated queries, so that the largest q.k has
+  // the largest score
+  const uint32_t flip = a.scale < 0 ? 0x80008000u : 0u;
+  const float scale = fmaxf(fabsf(a.scale), 1.17549435e-38f);  // not 0: -inf * 0
+  uint4 qf[KD];
+#pragma unroll
+  for (int s = 0; s < KD; ++s) {
+    const int d = 16 * s + 8 * h2;
+    qf[s] = d < a.D ? *(const uint4*)(qp + d * 2) : make_uint4(0, 0, 0, 0);
+    qf[s].x ^= flip;
+    qf[s].y ^= flip;
+    qf[s].z ^= flip;
+    qf[s].w ^= flip;
+  }
+
+  f32x16 o[DT];
+#pragma unroll
+  for (int j = 0; j < DT; ++j) o[j] = (f32x16)(0.f);
+  float m = -INFINITY, l = 0.f;
+
+  // loads: piece lc of rows lr, lr + RSTEP, ...  Rows outside the tile's keys
+  // repeat its first or last one: they get no weight, but have to be finite.
+  const int lc = tid % CPR, lr = tid / CPR;
+  const bool lon = lc * 8 < a.D;
+  const int P1 = (1 << a.pshift) - 1;
+  const size_t hrow = (size_t)h << a.pshift;
+  const size_t vofs = ((size_t)a.Hkv << a.pshift) * rowb;
+  const int32_t* trow = a.table + (size_t)t.row.seq * a.M;
+  // a table that names no page somewhere in the tile's keys: those keys are
+  // looked up again and masked one by one
+  bool bad = false;
+  for (int j = (kbeg >> a.pshift) + tid; j <= (kend - 1) >> a.pshift; j += TILE_T)
+    bad |= trow[j] < 0 || trow[j] >= a.N;
+  bad = __syncthreads_or(bad);
+  if (bad && tid == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
+  uint4 sk[NL], sv[NL];
+  auto key_of = [&](int base, int i) { return max(kbeg, min(base + lr + i * RSTEP, kend - 1)); };
+  int page[NL];
+  auto load_pages = [&](int base) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) page[i] = trow[key_of(base, i) >> a.pshift];
+  };
+  auto load_rows = [&](int base) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int key = key_of(base, i);
+      const char* p = a.pool + (int64_t)page[i] * (int64_t)a.page_bytes + (hrow + (key & P1)) * rowb + lc * 16;
+      const char* pv = p + vofs;
+      if (bad && (page[i] < 0 || page[i] >= a.N))  // masked below: any finite row will do
+        p = pv = a.q + (int64_t)t.row.begin * a.q_stride + lc * 16;
+      sk[i] = lon ? *(const uint4*)p : make_uint4(0, 0, 0, 0);
+      sv[i] = lon ? *(const uint4*)pv : make_uint4(0, 0, 0, 0);
+    }
+  };
+  auto store_rows = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int row = lr + i * RSTEP;
+      s_k[buf][row * CPR + C::kperm(row, lc)] = sk[i];
+      s_v[buf][row * CPR + C::vperm(row, lc)] = sv[i];
+    }
+  };
+
+  const int k0 = kbeg / KB * KB;
+  if (kend > 0) load_pages(k0);
+  if (kend > 0) {
+    load_rows(k0);
+    load_pages(k0 + KB);
+    store_rows(0);
+  }
+  __syncthreads();
+  int buf = 0;
+  for (int base = k0; base < kend; base += KB, buf ^= 1) {
+    const bool more = base + KB < kend;
+    if (more) {
+      load_rows(base + KB);
+      load_pages(base + 2 * KB);
+    }
+    if (base <= wmax && (a.window == 0 || base + KB - 1 > wmin - a.window)) {
+      const bool full = !bad && base + KB - 1 <= wmin && (a.window == 0 || base > wmax - a.window);
+      f32x16 sc[KT];
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        sc[kt] = (f32x16)(0.f);
+        const int row = 32 * kt + r;
+#pragma unroll
+        for (int s = 0; s < KD; ++s)
+          sc[kt] = mfma32<T>(s_k[buf][row * CPR + C::kperm(row, 2 * s + h2)], qf[s], sc[kt]);
+      }
+      if (!full) {
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = base + 32 * kt + 8 * (i / 4) + 4 * h2 + i % 4;
+            if (key > qpos || (a.window && key <= qpos - a.window)) sc[kt][i] = -INFINITY;
+            if (bad && sc[kt][i] != -INFINITY) {
+              const int p = trow[key >> a.pshift];  // key <= qpos: in the table
+              if (p < 0 || p >= a.N) sc[kt][i] = -INFINITY;
+            }
+          }
+      }
+      float mx = sc[0][0];
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[kt][i]);
+      {
+        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx),
+                                                        false, false);
+        mx = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])) * scale;
+      }
+      if (__any(mx > m)) {
+        const float mn = fmaxf(m, mx);
+        const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int j = 0; j < DT; ++j) o[j] *= alpha;
+      }
+      const float mu = m == -INFINITY ? 0.f : m;
+      uint4 pf[2 * KT];
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        uint32_t u[8];
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kt][i], scale, -mu));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kt][i + 1], scale, -mu));
+          l += p0 + p1;
+          u[i / 2] = pack2<T>(p0, p1);  // rounded to w, as the matrix cores take it
+        }
+        pf[2 * kt] = make_uint4(u[0], u[1], u[2], u[3]);
+        pf[2 * kt + 1] = make_uint4(u[4], u[5], u[6], u[7]);
+      }
+      // V^T: rows 32 j + l % 32, keys 16 mm + 4 h + {0..3} and 8 further
+      const int vr = 4 * h2 + (lane >> 2 & 3), vc = 16 * (lane >> 4 & 1) + 4 * (lane & 3);
+#pragma unroll
+      for (int mm = 0; mm < 2 * KT; ++mm)
+#pragma unroll
+        for (int j = 0; j < DT; ++j) {
+          const int ra = 16 * mm + vr, rb = ra + 8, d = 32 * j + vc;
+          typedef __attribute__((address_space(3))) s16x4 lds4;
+          const char* vb = (const char*)s_v[buf];
+          const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (lds4*)(vb + (ra * CPR + C::vperm(ra, d / 8)) * 16 + (d & 4) * 2));
+          const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (lds4*)(vb + (rb * CPR + C::vperm(rb, d / 8)) * 16 + (d & 4) * 2));
+          const uint2 xu = __builtin_bit_cast(uint2, x), yu = __builtin_bit_cast(uint2, y);
+          o[j] = mfma32<T>(make_uint4(xu.x, xu.y, yu.x, yu.y), pf[mm], o[j]);
+        }
+    }
+    if (more) store_rows(buf ^ 1);
+    __syncthreads();
+  }
+
+  l = swap32_add(l, l);
+  if (wave * 32 + r >= t.nrow) return;
+  const bool none = m == -INFINITY;  // a row that sees nothing is zero
+  const float inv = 1.f / l;
+  char* op = a.out + (int64_t)(t.row.begin + tok) * a.out_stride + (int64_t)head * rowb;
+#pragma unroll
+  for (int j = 0; j < DT; ++j)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const int d = 32 * j + 2 * i + 4 * h2;
+      if (d >= a.D) continue;
+      *(uint2*)(op + d * 2) =
+          none ? make_uint2(0, 0)
+               : make_uint2(pack2<T>(o[j][i] * inv, o[j][i + 1] * inv),
+                            pack2<T>(o[j][i + 2] * inv, o[j][i + 3] * inv));
+    }
+}
+
+template <class T, int DP>
+hipError_t launch_tile(AttnArgs a, hipStream_t stream) {
+  a.tiles = a.b.cu ? (int)((int64_t)a.b.n_tokens * a.G / TB) + a.b.n_seq
+                   : a.b.n_seq * ((a.G + TB - 1) / TB);
+  hipLaunchKernelGGL((attn_tile_kernel<T, DP>), dim3((unsigned)((int64_t)a.tiles * a.Hkv)),
+                     dim3(TILE_T), 0, stream, a);
+  return hipGetLastError();
+}
+
 template <class T, int DP>
 hipError_t launch_rows(AttnArgs a, int64_t keys, hipStream_t stream) {
   // enough workgroups to fill the card, at least 128 keys (one step of each
@@ -493,7 +755,14 @@ hipError_t launch_rows(AttnArgs a, int64_t keys, hipStream_t stream) {
 }
 
 template <class T>
-hipError_t launch_attn_t(AttnArgs& a, int64_t keys, hipStream_t stream) {
+hipError_t launch_attn_t(AttnArgs& a, int64_t keys, int max_tokens, hipStream_t stream) {
+  if constexpr (T::V == 8) {
+    if (a.b.cu && (int64_t)max_tokens * a.G > 64) {
+      if (a.D <= 64) return launch_tile<T, 64>(a, stream);
+      if (a.D <= 128) return launch_tile<T, 128>(a, stream);
+      return launch_tile<T, 256>(a, stream);
+    }
+  }
   if (a.D <= 64) return launch_rows<T, 64>(a, keys, stream);
   if (a.D <= 128) return launch_rows<T, 128>(a, keys, stream);
   return launch_rows<T, 256>(a, keys, stream);
@@ -536,9 +805,9 @@ hipError_t launch_attn(const np_kv_shape& s, int layer, const np_kv_batch& b,
   int64_t keys = a.b.lim;
   if (window > 0) keys = std::min<int64_t>(keys, (int64_t)window + RB + 32);
   keys = std::max<int64_t>(keys, 1);
-  if (s.dtype == NP_F32) return launch_attn_t<TF32>(a, keys, stream);
-  if (s.dtype == NP_F16) return launch_attn_t<TF16>(a, keys, stream);
-  return launch_attn_t<TBF16>(a, keys, stream);
+  if (s.dtype == NP_F32) return launch_attn_t<TF32>(a, keys, b.max_tokens, stream);
+  if (s.dtype == NP_F16) return launch_attn_t<TF16>(a, keys, b.max_tokens, stream);
+  return launch_attn_t<TBF16>(a, keys, b.max_tokens, stream);
 }
 
 }  // namespace np

@@ -29,8 +29,7 @@
  *  w = dtype of queries, keys, values and outputs.
  *  Requirements: L >= 1; Hkv divides Hq <= 1024; D a multiple of 8, 8..256;
  *  P one of 16, 32, 64, 128, 256; 1 <= N <= 2^20; 1 <= S <= 4096; M >= 1 and
- *  M * P <= 2^30; a page of one layer (2 Hkv P D sizeof(w)) below 2 GiB.
- *  Any violation is NP_ERR_INVALID_ARG.
+ *  M * P <= 2^30.  Any violation is NP_ERR_INVALID_ARG.
  *
  *  pool [L][N][2][Hkv][P][D] of type w, device: page p of layer l holds the
  *  keys ([0]) and the values ([1]) of P consecutive positions of a sequence,
@@ -84,9 +83,10 @@ typedef struct np_kv_state {
  * The arrays are device int32, 4-byte aligned; each may change between calls
  * without the host knowing.  Device-side checks: a sequence outside [0, S), a
  * cu_tokens that descends or leaves [0, n_tokens], and a position at or past
- * max_len or M P set NP_DEVERR_STATE (the row is then not served); a page
- * outside [0, N) where a token sees keys sets NP_DEVERR_NOT_RESIDENT (its
- * keys count as not visible). */
+ * max_len or M P set NP_DEVERR_STATE, and the row is not served (one whose
+ * cu_tokens are bad has no tokens); a page outside [0, N) where a token sees
+ * keys sets NP_DEVERR_NOT_RESIDENT (its keys count as not visible).  At most
+ * 2^24 tokens and 2^30 query heads in all. */
 typedef struct np_kv_batch {
   int32_t n_seq;
   int32_t n_tokens;

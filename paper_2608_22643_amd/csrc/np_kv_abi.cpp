@@ -29,8 +29,6 @@ static np_status check_kv_shape(const np_kv_shape* s) {
     return fail(NP_ERR_INVALID_ARG, "max_seqs %d outside [1, %d]", s->max_seqs, KV_MAX_SEQS);
   if (s->seq_pages < 1 || (int64_t)s->seq_pages * P > ((int64_t)1 << 30))
     return fail(NP_ERR_INVALID_ARG, "seq_pages %d: positions outside [1, 2^30]", s->seq_pages);
-  if (kv_page_bytes(*s) >= ((size_t)1 << 31))
-    return fail(NP_ERR_INVALID_ARG, "a page of one layer must stay below 2 GiB");
   return NP_OK;
 }
 

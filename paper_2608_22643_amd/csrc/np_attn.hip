@@ -88,7 +88,11 @@ __device__ inline bool find_tile(const KvBatch& b, int G, int tile, int32_t* err
   }
   row = __builtin_amdgcn_readfirstlane(row);
   blk = __builtin_amdgcn_readfirstlane(blk);
-  t->row = kv_row(b, row, threadIdx.x == 0 ? err : nullptr);
+  const KvRow r = kv_row(b, row, threadIdx.x == 0 ? err : nullptr);
+  t->row.begin = __builtin_amdgcn_readfirstlane(r.begin);  // the same in every lane
+  t->row.n = __builtin_amdgcn_readfirstlane(r.n);
+  t->row.p0 = __builtin_amdgcn_readfirstlane(r.p0);
+  t->row.seq = __builtin_amdgcn_readfirstlane(r.seq);
   t->rho0 = blk * RB;
   t->nrow = min(RB, t->row.n * G - t->rho0);
   if (t->nrow <= 0) return false;
@@ -108,6 +112,11 @@ __device__ inline uint32_t pack2(float a, float b) {
   else
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf162_t));
 }
+
+// 16 bytes of global memory (an address the compiler cannot trace to an
+// argument would become a flat load, which waits for LDS too)
+typedef const __attribute__((address_space(1))) u32x4_t* global16_t;
+__device__ inline u32x4_t load_global16(const char* p) { return *(global16_t)(uintptr_t)p; }
 
 __device__ inline float max_groups(float v) {  // over lanes l, l ^ 16, l ^ 32, l ^ 48
   auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -153,7 +162,7 @@ struct RowsCfg {
 };
 
 template <class T, int DP>
-__global__ __launch_bounds__(ROWS_T) void attn_rows_kernel(AttnArgs a) {
+__global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(AttnArgs a) {
   using C = RowsCfg<T, DP>;
   constexpr int V = C::V, W = C::W, KS = C::KS, KT = C::KT, KD = C::KD, NV = C::NV, VS = C::VS,
                 VR = C::VR;
@@ -523,13 +532,14 @@ struct TileCfg {
   }
 };
 
-template <class T, int DP>
-__global__ __launch_bounds__(TILE_T) void attn_tile_kernel(AttnArgs a) {
+// FULL: D == DP; otherwise the pieces past D stay zero in LDS.
+template <class T, int DP, bool FULL>
+__global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(AttnArgs a) {
   using C = TileCfg<DP>;
   constexpr int KB = C::KB, CPR = C::CPR, NL = C::NL, RSTEP = C::RSTEP;
   constexpr int KT = KB / 32, KD = DP / 16, DT = DP / 32;
-  __shared__ uint4 s_k[2][KB * CPR];
-  __shared__ uint4 s_v[2][KB * CPR];
+  __shared__ u32x4_t s_k[2][KB * CPR];
+  __shared__ u32x4_t s_v[2][KB * CPR];
 
   const int tid = threadIdx.x, lane = tid % WAVE;
   const int wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
@@ -574,19 +584,20 @@ __global__ __launch_bounds__(TILE_T) void attn_tile_kernel(AttnArgs a) {
   // loads: piece lc of rows lr, lr + RSTEP, ...  Rows outside the tile's keys
   // repeat its first or last one: they get no weight, but have to be finite.
   const int lc = tid % CPR, lr = tid / CPR;
-  const bool lon = lc * 8 < a.D;
+  const bool lon = FULL || lc * 8 < a.D;
   const int P1 = (1 << a.pshift) - 1;
   const size_t hrow = (size_t)h << a.pshift;
   const size_t vofs = ((size_t)a.Hkv << a.pshift) * rowb;
+  const char* hpool = a.pool + hrow * rowb + lc * 16;
   const int32_t* trow = a.table + (size_t)t.row.seq * a.M;
   // a table that names no page somewhere in the tile's keys: those keys are
   // looked up again and masked one by one
-  bool bad = false;
+  int any_bad = 0;
   for (int j = (kbeg >> a.pshift) + tid; j <= (kend - 1) >> a.pshift; j += TILE_T)
-    bad |= trow[j] < 0 || trow[j] >= a.N;
-  bad = __syncthreads_or(bad);
+    any_bad |= trow[j] < 0 || trow[j] >= a.N;
+  const bool bad = __builtin_amdgcn_readfirstlane(__syncthreads_or(any_bad)) != 0;
   if (bad && tid == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
-  uint4 sk[NL], sv[NL];
+  u32x4_t sk[NL] = {}, sv[NL] = {};
   auto key_of = [&](int base, int i) { return max(kbeg, min(base + lr + i * RSTEP, kend - 1)); };
   int page[NL];
   auto load_pages = [&](int base) {
@@ -594,25 +605,50 @@ __global__ __launch_bounds__(TILE_T) void attn_tile_kernel(AttnArgs a) {
     for (int i = 0; i < NL; ++i) page[i] = trow[key_of(base, i) >> a.pshift];
   };
   auto load_rows = [&](int base) {
+    const char* p[NL];
+    int64_t vo[NL];
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int key = key_of(base, i);
-      const char* p = a.pool + (int64_t)page[i] * (int64_t)a.page_bytes + (hrow + (key & P1)) * rowb + lc * 16;
-      const char* pv = p + vofs;
-      if (bad && (page[i] < 0 || page[i] >= a.N))  // masked below: any finite row will do
-        p = pv = a.q + (int64_t)t.row.begin * a.q_stride + lc * 16;
-      sk[i] = lon ? *(const uint4*)p : make_uint4(0, 0, 0, 0);
-      sv[i] = lon ? *(const uint4*)pv : make_uint4(0, 0, 0, 0);
+      p[i] = hpool + (int64_t)page[i] * (int64_t)a.page_bytes + (key_of(base, i) & P1) * rowb;
+      vo[i] = vofs;
+    }
+    if (bad)
+#pragma unroll
+      for (int i = 0; i < NL; ++i)
+        if (page[i] < 0 || page[i] >= a.N) {  // masked below: any finite row will do
+          p[i] = a.q + (int64_t)t.row.begin * a.q_stride + lc * 16;
+          vo[i] = 0;
+        }
+    if (lon) {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        sk[i] = load_global16(p[i]);
+        sv[i] = load_global16(p[i] + vo[i]);
+      }
     }
   };
   auto store_rows = [&](int buf) {
+    if (lon) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int row = lr + i * RSTEP;
-      s_k[buf][row * CPR + C::kperm(row, lc)] = sk[i];
-      s_v[buf][row * CPR + C::vperm(row, lc)] = sv[i];
+      for (int i = 0; i < NL; ++i) {
+        const int row = lr + i * RSTEP;
+        s_k[buf][row * CPR + C::kperm(row, lc)] = sk[i];
+        s_v[buf][row * CPR + C::vperm(row, lc)] = sv[i];
+      }
     }
   };
+  if constexpr (!FULL) {
+    if (!lon)
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int row = lr + i * RSTEP;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          s_k[x][row * CPR + C::kperm(row, lc)] = (u32x4_t)(0u);
+          s_v[x][row * CPR + C::vperm(row, lc)] = (u32x4_t)(0u);
+        }
+      }
+  }
 
   const int k0 = kbeg / KB * KB;
   if (kend > 0) load_pages(k0);
@@ -638,7 +674,7 @@ __global__ __launch_bounds__(TILE_T) void attn_tile_kernel(AttnArgs a) {
         const int row = 32 * kt + r;
 #pragma unroll
         for (int s = 0; s < KD; ++s)
-          sc[kt] = mfma32<T>(s_k[buf][row * CPR + C::kperm(row, 2 * s + h2)], qf[s], sc[kt]);
+          sc[kt] = mfma32<T>(as_uint4(s_k[buf][row * CPR + C::kperm(row, 2 * s + h2)]), qf[s], sc[kt]);
       }
       if (!full) {
 #pragma unroll
@@ -647,11 +683,14 @@ __global__ __launch_bounds__(TILE_T) void attn_tile_kernel(AttnArgs a) {
           for (int i = 0; i < 16; ++i) {
             const int key = base + 32 * kt + 8 * (i / 4) + 4 * h2 + i % 4;
             if (key > qpos || (a.window && key <= qpos - a.window)) sc[kt][i] = -INFINITY;
-            if (bad && sc[kt][i] != -INFINITY) {
-              const int p = trow[key >> a.pshift];  // key <= qpos: in the table
+          }
+        if (bad)
+          for (int kt = 0; kt < KT; ++kt)
+            for (int i = 0; i < 16; ++i) {
+              const int key = base + 32 * kt + 8 * (i / 4) + 4 * h2 + i % 4;
+              const int p = trow[min(key, kend - 1) >> a.pshift];
               if (p < 0 || p >= a.N) sc[kt][i] = -INFINITY;
             }
-          }
       }
       float mx = sc[0][0];
 #pragma unroll
@@ -729,8 +768,11 @@ template <class T, int DP>
 hipError_t launch_tile(AttnArgs a, hipStream_t stream) {
   a.tiles = a.b.cu ? (int)((int64_t)a.b.n_tokens * a.G / TB) + a.b.n_seq
                    : a.b.n_seq * ((a.G + TB - 1) / TB);
-  hipLaunchKernelGGL((attn_tile_kernel<T, DP>), dim3((unsigned)((int64_t)a.tiles * a.Hkv)),
-                     dim3(TILE_T), 0, stream, a);
+  const dim3 grid((unsigned)((int64_t)a.tiles * a.Hkv));
+  if (a.D == DP)
+    hipLaunchKernelGGL((attn_tile_kernel<T, DP, true>), grid, dim3(TILE_T), 0, stream, a);
+  else
+    hipLaunchKernelGGL((attn_tile_kernel<T, DP, false>), grid, dim3(TILE_T), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -11,6 +11,7 @@
 // is a (token, head of the group) pair and a block of rows reads each key and
 // value once.
 #include <algorithm>
+#include <type_traits>
 
 #include "np_kv.hpp"
 
@@ -36,6 +37,9 @@ struct AttnArgs {
   int chunk;  // keys per split, a multiple of 128
   int splits;
   float *part, *ml;
+  const char* zeros;  // KV_ZEROS bytes
+  int* count;         // arrivals of a block's splits, 0 between calls
+  int prow;  // rows of a block that have partials: min(16, G) with one token a row
   int32_t* err;
 };
 
@@ -117,6 +121,9 @@ __device__ inline uint32_t pack2(float a, float b) {
 // argument would become a flat load, which waits for LDS too)
 typedef const __attribute__((address_space(1))) u32x4_t* global16_t;
 __device__ inline u32x4_t load_global16(const char* p) { return *(global16_t)(uintptr_t)p; }
+typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
+typedef const __attribute__((address_space(1))) u32x2_t* global8_t;
+__device__ inline u32x2_t load_global8(const char* p) { return *(global8_t)(uintptr_t)p; }
 
 __device__ inline float max_groups(float v) {  // over lanes l, l ^ 16, l ^ 32, l ^ 48
   auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -147,6 +154,7 @@ __device__ inline float sum_groups(float v) {
 constexpr int RB = 16;
 constexpr int NWAVE = 4;
 constexpr int ROWS_T = NWAVE * WAVE;
+constexpr int MAX_SPLITS = 128;
 
 template <class T, int DP>
 struct RowsCfg {
@@ -161,8 +169,11 @@ struct RowsCfg {
   static constexpr int OP = DP + 4;              // LDS row of outputs, padded
 };
 
-template <class T, int DP>
-__global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(AttnArgs a) {
+// FULL: D == DP; otherwise the key pieces past D are zeroed (a piece inside D is
+// read in their place), and the output columns past D are not stored.
+template <class T, int DP, bool FULL>
+__global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(
+    AttnArgs a) {
   using C = RowsCfg<T, DP>;
   constexpr int V = C::V, W = C::W, KS = C::KS, KT = C::KT, KD = C::KD, NV = C::NV, VS = C::VS,
                 VR = C::VR;
@@ -175,8 +186,7 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(At
   const int id = blockIdx.x;
   const int h = id % a.Hkv, tile = id / a.Hkv % a.tiles, split = id / a.Hkv / a.tiles;
   Tile t;
-  if (!find_tile<RB>(a.b, a.G, tile, split == 0 && h == 0 ? a.err : nullptr, &t))
-    return;
+  if (!find_tile<RB>(a.b, a.G, tile, split == 0 && h == 0 ? a.err : nullptr, &t)) return;
 
   const int kbeg = a.window && t.maxpos >= 0 ? max(0, t.minpos - a.window + 1) : 0;
   const int kend = t.maxpos + 1;
@@ -185,6 +195,24 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(At
   if (split >= ns) return;
   const int k0 = kal + split * a.chunk;
   const int k1 = split + 1 < ns ? k0 + a.chunk : kend;
+
+  // page ids through the scalar cache: uniform, and counted apart from the
+  // vector loads in flight.  A step of 32 keys has two pages when P is 16.
+  typedef const __attribute__((address_space(4))) int32_t* table_t;
+  const table_t trow = (table_t)(uintptr_t)(a.table + (size_t)t.row.seq * a.M);
+  const int klast = max(kend - 1, 0);
+  struct Pages {
+    int a, b;
+  };
+  auto pages_of = [&](int base) {
+    Pages p;
+    p.a = trow[max(kbeg, min(base, klast)) >> a.pshift];
+    p.b = KS == 32 ? trow[max(kbeg, min(base + 16, klast)) >> a.pshift] : p.a;
+    return p;
+  };
+  int base = k0 + wave * KS;
+  Pages pg = {0, 0};
+  if (base < k1) pg = pages_of(base);
 
   // this lane's query (B operand): column r, d = 4 V s + V g
   const int rr = min(r, t.nrow - 1);
@@ -196,7 +224,7 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(At
 #pragma unroll
     for (int s = 0; s < KD; ++s) {
       const int d = 4 * V * s + V * g;
-      qf[s] = d < a.D ? *(const uint4*)(qp + d * W) : make_uint4(0, 0, 0, 0);
+      qf[s] = FULL || d < a.D ? *(const uint4*)(qp + d * W) : make_uint4(0, 0, 0, 0);
     }
   }
 
@@ -208,107 +236,117 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(At
   float m = -INFINITY, l = 0.f;
 
   const int P1 = (1 << a.pshift) - 1;
-  const size_t hb = (size_t)h << a.pshift;  // rows before head h in a page's keys
-  const size_t vb = (size_t)a.Hkv << a.pshift;
-  const int32_t* trow = a.table + (size_t)t.row.seq * a.M;
   const int rowb = a.D * W;
+  const char* kpool = a.pool + ((size_t)h << a.pshift) * rowb;
+  const size_t vofs = ((size_t)a.Hkv << a.pshift) * rowb;
 
   // keys of a lane: A-operand row r of tile kt is key kk + 4 kt (16-bit) or r
   const int kk = V == 8 ? 8 * (r >> 2) + (r & 3) : r;
   const int vk = VR * g;  // first value row of the lane
+  // byte offsets of the lane's pieces in a row
+  int kd[KD], vd[VS];
+#pragma unroll
+  for (int s = 0; s < KD; ++s) {
+    const int d = 4 * V * s + V * g;
+    kd[s] = (FULL || d < a.D ? d : 0) * W;
+  }
+#pragma unroll
+  for (int s = 0; s < VS; ++s) {
+    const int d = 16 * NV * s + NV * r;
+    vd[s] = (FULL || d < a.D ? d : 0) * W;
+  }
 
-  uint4 kf[KT][KD];
-  uint32_t vf[VR][VS][NV * W / 4];
-  int okbits = 0;  // which 16-key halves of the loaded step have a page
+  u32x4_t kf[KT][KD];
+  u32x4_t vf[VR][VS];  // 8 bytes of each used when NV W is 8
+  int ok = 0, next_ok = 0;  // which 16-key halves of a step have a page
+  bool missing = false;     // a bad table entry among the keys
+  const char* vptr;
+  uint32_t vrow[VR];
 
-  // page of key `key` (uniform), or -1: beyond the keys of this block (no
-  // error) or a bad table entry
-  auto page_of = [&](int key) -> int {
-    if (key >= kend) return -1;
-    const int p = trow[key >> a.pshift];
-    if (p < 0 || p >= a.N) {
-      if (threadIdx.x % WAVE == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
-      return -1;
+  // Addresses of a step.  A half without a page (a bad table entry) is read
+  // from zeros and masked.  Value rows outside [kbeg, kend) repeat the first or
+  // the last one inside: they get no weight, but memory there may hold
+  // anything, and 0 * NaN would reach the output.
+  auto load_k = [&](int base, Pages p) {
+    const bool ha = (uint32_t)p.a < (uint32_t)a.N, hb = (uint32_t)p.b < (uint32_t)a.N;
+    next_ok = (ha ? 1 : 0) | (hb ? 2 : 0);
+    const bool hk = V == 8 && r >= 8 ? hb : ha, hv = V == 8 && g >= 2 ? hb : ha;
+    const int pk = V == 8 && r >= 8 ? p.b : p.a, pv = V == 8 && g >= 2 ? p.b : p.a;
+    const char* kptr = kpool + (int64_t)pk * (int64_t)a.page_bytes + ((base + kk) & P1) * rowb;
+    vptr = kpool + vofs + (int64_t)pv * (int64_t)a.page_bytes;
+    if (!hk) kptr = a.zeros;
+    if (!hv) vptr = a.zeros;
+    if (base >= kbeg && base + KS <= kend) {
+#pragma unroll
+      for (int e = 0; e < VR; ++e) vrow[e] = hv ? (((base + vk) & P1) + e) * rowb : 0;
+    } else {
+#pragma unroll
+      for (int e = 0; e < VR; ++e)
+        vrow[e] = hv ? (max(kbeg, min(base + vk + e, klast)) & P1) * rowb : 0;
     }
-    return p;
-  };
-  const char *kptr, *vptr;
-  auto locate = [&](int base) {
-    const int pa = page_of(base);
-    int pb = pa;
-    if constexpr (KS == 32) {
-      if (a.pshift == 4) pb = page_of(base + 16);
-    }
-    okbits = (pa >= 0 ? 1 : 0) | (pb >= 0 ? 2 : 0);
-    // a missing half is read from page 0 and masked
-    const int pk = max(0, V == 8 && r >= 8 ? pb : pa), pv = max(0, V == 8 && g >= 2 ? pb : pa);
-    kptr = a.pool + (size_t)pk * a.page_bytes + (hb + ((base + kk) & P1)) * rowb;
-    vptr = a.pool + (size_t)pv * a.page_bytes + (vb + hb + ((base + vk) & P1)) * rowb;
-  };
-  auto load_k = [&]() {
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-      for (int s = 0; s < KD; ++s) {
-        const int d = 4 * V * s + V * g;
-        kf[kt][s] = d < a.D ? *(const uint4*)(kptr + 4 * kt * rowb + d * W) : make_uint4(0, 0, 0, 0);
-      }
+      for (int s = 0; s < KD; ++s) kf[kt][s] = load_global16(kptr + 4 * kt * rowb + kd[s]);
   };
   auto load_v = [&]() {
 #pragma unroll
     for (int e = 0; e < VR; ++e)
 #pragma unroll
       for (int s = 0; s < VS; ++s) {
-        const int d = 16 * NV * s + NV * r;
+        const char* p = vptr + vrow[e] + vd[s];
         if constexpr (NV * W == 16) {
-          const uint4 x = d < a.D ? *(const uint4*)(vptr + e * rowb + d * W) : make_uint4(0, 0, 0, 0);
-          vf[e][s][0] = x.x;
-          vf[e][s][1] = x.y;
-          vf[e][s][2] = x.z;
-          vf[e][s][3] = x.w;
+          vf[e][s] = load_global16(p);
         } else {
-          const uint2 x = d < a.D ? *(const uint2*)(vptr + e * rowb + d * W) : make_uint2(0, 0);
-          vf[e][s][0] = x.x;
-          vf[e][s][1] = x.y;
+          const u32x2_t x = load_global8(p);
+          vf[e][s].x = x.x;
+          vf[e][s].y = x.y;
         }
       }
   };
 
-  int base = k0 + wave * KS;
-  if (base < k1) {
-    locate(base);
-    load_k();
+  // One step.  LAST: no step of this wave follows.  Its values are asked for
+  // while its keys are on their way, the next step's keys as soon as this
+  // one's are used, so that loads are in flight during all of the arithmetic.
+  auto step = [&](auto last) {
+    constexpr bool LAST = decltype(last)::value;
+    const int next = base + NWAVE * KS;
     load_v();
-  }
-  for (; base < k1; base += NWAVE * KS) {
-    const int ok = okbits;
+    __builtin_amdgcn_sched_barrier(0);
     const bool full = ok == 3 && base + KS - 1 <= t.minpos &&
                       (a.window == 0 || base > t.maxpos - a.window);
-    const bool more = base + NWAVE * KS < k1;
     f32x4 sc[KT];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
       sc[kt] = (f32x4)(0.f);
 #pragma unroll
-      for (int s = 0; s < KD; ++s) sc[kt] = mfma_step<T>(kf[kt][s], qf[s], sc[kt]);
+      for (int s = 0; s < KD; ++s) {
+        u32x4_t k = kf[kt][s];
+        if (!FULL && 4 * V * s + V * g >= a.D) k = (u32x4_t)(0u);
+        sc[kt] = mfma_step<T>(as_uint4(k), qf[s], sc[kt]);
+      }
     }
-    if (more) {
-      locate(base + NWAVE * KS);
-      load_k();
+    if constexpr (!LAST) {
+      // kept behind the products: earlier, the new keys would need registers
+      // of their own
+      __builtin_amdgcn_sched_barrier(0);
+      load_k(next, pg);
+      pg = pages_of(next + NWAVE * KS);
     }
     // scores of key base + vk + 4 kt + i
     float p[4 * KT];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        p[4 * kt + i] = sc[kt][i] * a.scale;
-        if (!full) {
-          const int key = base + vk + 4 * kt + i;
-          const bool has = (ok >> (KS == 32 && g >= 2 ? 1 : 0)) & 1;
-          if (!has || key > qpos || (a.window && key <= qpos - a.window)) p[4 * kt + i] = -INFINITY;
-        }
+      for (int i = 0; i < 4; ++i) p[4 * kt + i] = sc[kt][i] * a.scale;
+    const bool has = (ok >> (KS == 32 && g >= 2 ? 1 : 0)) & 1;
+    if (!full) {
+#pragma unroll
+      for (int i = 0; i < 4 * KT; ++i) {
+        const int key = base + vk + i;
+        if (!has || key > qpos || (a.window && key <= qpos - a.window)) p[i] = -INFINITY;
       }
+    }
     float mx = p[0];
 #pragma unroll
     for (int i = 1; i < 4 * KT; ++i) mx = fmaxf(mx, p[i]);
@@ -341,29 +379,14 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(At
       pb = make_uint4(__float_as_uint(p[0]), __float_as_uint(p[1]), __float_as_uint(p[2]),
                       __float_as_uint(p[3]));
     }
-    if (!full) {
-      // values no row of the block sees must not meet the products: memory
-      // past a sequence's end may hold anything (0 * NaN)
-      const bool has = (ok >> (KS == 32 && g >= 2 ? 1 : 0)) & 1;
-#pragma unroll
-      for (int e = 0; e < VR; ++e) {
-        const int key = base + vk + e;
-        if (!has || key < kbeg || key >= kend) {
-#pragma unroll
-          for (int s = 0; s < VS; ++s)
-#pragma unroll
-            for (int x = 0; x < NV * W / 4; ++x) vf[e][s][x] = 0;
-        }
-      }
-    }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int s = 0; s < VS; ++s)
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         uint4 av;
         if constexpr (V == 8) {
-          constexpr uint32_t LO = 0x05040100u, HI = 0x07060302u;
-          const uint32_t sel = j & 1 ? HI : LO;
+          const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;  // high or low halves
           av.x = __builtin_amdgcn_perm(vf[1][s][j / 2], vf[0][s][j / 2], sel);
           av.y = __builtin_amdgcn_perm(vf[3][s][j / 2], vf[2][s][j / 2], sel);
           av.z = __builtin_amdgcn_perm(vf[5][s][j / 2], vf[4][s][j / 2], sel);
@@ -373,8 +396,25 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(At
         }
         o[s][j] = mfma_step<T>(av, pb, o[s][j]);
       }
-    if (more) load_v();
+    if constexpr (!LAST) {
+      ok = next_ok;
+      missing |= ok != 3;
+      base = next;
+    }
+  };
+
+  if (base < k1) {
+    load_k(base, pg);
+    ok = next_ok;
+    missing |= ok != 3;
+    pg = pages_of(base + NWAVE * KS);
+    if (base + NWAVE * KS < k1) {
+      do step(std::false_type{});
+      while (base + NWAVE * KS < k1);
+    }
+    step(std::true_type{});
   }
+  if (missing && lane == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
 
   // the four waves' results meet in LDS
   l = sum_groups(l);
@@ -391,9 +431,24 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(At
         *(float4*)&s_o[wave][r][16 * NV * s + NV * (4 * g + i) + j] =
             make_float4(o[s][j][i], o[s][j + 1][i], o[s][j + 2][i], o[s][j + 3][i]);
   __syncthreads();
-  const size_t slot = ((size_t)tile * a.Hkv + h) * a.splits + split;
-  for (int u = threadIdx.x; u < t.nrow * (DP / 4); u += ROWS_T) {
-    const int qr = u / (DP / 4), d = u % (DP / 4) * 4;
+  auto store_out = [&](int qr, int d, float4 sum, float L) {
+    const float inv = 1.f / L;
+    const bool none = L == 0.f;  // a row that sees nothing is zero
+    const float f[4] = {none ? 0.f : sum.x * inv, none ? 0.f : sum.y * inv,
+                        none ? 0.f : sum.z * inv, none ? 0.f : sum.w * inv};
+    const int rho = t.rho0 + qr;
+    char* op = a.out + (int64_t)(t.row.begin + rho / a.G) * a.out_stride +
+               ((int64_t)(h * a.G + rho % a.G) * a.D + d) * W;
+    if constexpr (V == 8)
+      *(uint2*)op = make_uint2(pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]));
+    else
+      *(float4*)op = make_float4(f[0], f[1], f[2], f[3]);
+  };
+  constexpr int TD = DP / 4;
+  const int block = tile * a.Hkv + h;
+  const __amdgpu_buffer_rsrc_t prs = make_rsrc(a.part, (uint32_t)KV_PART_ROWS * DP * 4);
+  for (int u = threadIdx.x; u < t.nrow * TD; u += ROWS_T) {
+    const int qr = u / TD, d = u % TD * 4;
     float M = -INFINITY;
 #pragma unroll
     for (int w = 0; w < NWAVE; ++w) M = fmaxf(M, s_m[w][qr]);
@@ -401,90 +456,110 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(At
     float L = 0.f;
 #pragma unroll
     for (int w = 0; w < NWAVE; ++w) {
-      const float mw = s_m[w][qr];
-      const float f = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - M);
+      const float mw = s_m[w][qr], lw = s_l[w][qr];
+      // without a maximum the sum is 0, or NaN when every score was
+      const float f = mw == -INFINITY ? lw : __builtin_amdgcn_exp2f(mw - M);
       const float4 x = *(const float4*)&s_o[w][qr][d];
-      L += f * s_l[w][qr];
+      L += f * lw;
       sum.x += f * x.x;
       sum.y += f * x.y;
       sum.z += f * x.z;
       sum.w += f * x.w;
     }
     if (ns > 1) {
-      *(float4*)(a.part + (slot * RB + qr) * DP + d) = sum;
-      if (d == 0) {
-        a.ml[(slot * RB + qr) * 2] = M;
-        a.ml[(slot * RB + qr) * 2 + 1] = L;
-      }
+      const uint32_t row = ((uint32_t)block * a.splits + split) * a.prow + qr;
+      buf_store16_agent(prs, (row * DP + d) * 4, sum);
+      if (d == 0)
+        __hip_atomic_store((uint64_t*)a.ml + row,
+                           (uint64_t)__float_as_uint(L) << 32 | __float_as_uint(M),
+                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     } else if (d < a.D) {
-      const float inv = M == -INFINITY ? 0.f : 1.f / L;  // a row that sees nothing is zero
-      const int rho = t.rho0 + qr;
-      char* op = a.out + (int64_t)(t.row.begin + rho / a.G) * a.out_stride +
-                 ((int64_t)(h * a.G + rho % a.G) * a.D + d) * W;
-      const float f[4] = {M == -INFINITY ? 0.f : sum.x * inv, M == -INFINITY ? 0.f : sum.y * inv,
-                          M == -INFINITY ? 0.f : sum.z * inv, M == -INFINITY ? 0.f : sum.w * inv};
-      if constexpr (V == 8)
-        *(uint2*)op = make_uint2(pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]));
-      else
-        *(float4*)op = make_float4(f[0], f[1], f[2], f[3]);
+      store_out(qr, d, sum, L);
     }
   }
-}
+  if (ns <= 1) return;
 
-// Joins the splits of a row: a workgroup per (row of a block, block and
-// head), DP / 4 threads over the row, the splits dealt to its other threads.
-template <class T, int DP>
-__global__ __launch_bounds__(ROWS_T) void attn_join_kernel(AttnArgs a) {
-  constexpr int W = 16 / T::V, KS = RowsCfg<T, DP>::KS;
-  constexpr int TD = DP / 4, SUB = ROWS_T / TD;
-  __shared__ float4 s_o[SUB][TD];
-  __shared__ float s_l[SUB];
-  const int h = blockIdx.x % a.Hkv, tile = blockIdx.x / a.Hkv, qr = blockIdx.y;
-  Tile t;
-  if (!find_tile<RB>(a.b, a.G, tile, nullptr, &t) || qr >= t.nrow) return;
-  const int kbeg = a.window && t.maxpos >= 0 ? max(0, t.minpos - a.window + 1) : 0;
-  const int kal = kbeg / KS * KS;
-  const int ns = min(a.splits, max(1, (t.maxpos + 1 - kal + a.chunk - 1) / a.chunk));
-  if (ns <= 1) return;  // written by the row kernel
-  const size_t slot = ((size_t)tile * a.Hkv + h) * a.splits;
-  const int x = threadIdx.x % TD, sub = threadIdx.x / TD;
-  float M = -INFINITY;
-  for (int c = 0; c < ns; ++c) M = fmaxf(M, a.ml[((slot + c) * RB + qr) * 2]);
-  float4 sum = make_float4(0, 0, 0, 0);
-  float L = 0.f;
-  for (int c = sub; c < ns; c += SUB) {
-    const float* ml = a.ml + ((slot + c) * RB + qr) * 2;
-    const float f = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - M);
-    const float4 v = *(const float4*)(a.part + ((slot + c) * RB + qr) * DP + x * 4);
-    L += f * ml[1];
-    sum.x += f * v.x;
-    sum.y += f * v.y;
-    sum.z += f * v.z;
-    sum.w += f * v.w;
-  }
-  s_o[sub][x] = sum;
-  if (x == 0) s_l[sub] = L;
+  // The last workgroup of a block to arrive joins its splits: the stores
+  // above go to the level that all XCDs share, and are complete before the
+  // count rises.  The order of the sums is that of the splits, whoever joins.
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if (sub || x * 4 >= a.D) return;
-  for (int i = 1; i < SUB; ++i) {
-    const float4 v = s_o[i][x];
-    sum.x += v.x;
-    sum.y += v.y;
-    sum.z += v.z;
-    sum.w += v.w;
-    L += s_l[i];
+  int* const s_last = (int*)&s_l[0][0];
+  if (threadIdx.x == 0) {
+    const int old = __hip_atomic_fetch_add(a.count + block, 1, __ATOMIC_RELAXED,
+                                           __HIP_MEMORY_SCOPE_AGENT);
+    *s_last = old == ns - 1;
+    if (old == ns - 1)  // for the next call
+      __hip_atomic_store(a.count + block, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-  const bool none = M == -INFINITY;
-  const float inv = 1.f / L;
-  const float f[4] = {none ? 0.f : sum.x * inv, none ? 0.f : sum.y * inv,
-                      none ? 0.f : sum.z * inv, none ? 0.f : sum.w * inv};
-  const int rho = t.rho0 + qr;
-  char* op = a.out + (int64_t)(t.row.begin + rho / a.G) * a.out_stride +
-             ((int64_t)(h * a.G + rho % a.G) * a.D + x * 4) * W;
-  if constexpr (T::V == 8)
-    *(uint2*)op = make_uint2(pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]));
-  else
-    *(float4*)op = make_float4(f[0], f[1], f[2], f[3]);
+  __syncthreads();
+  if (!*s_last) return;
+  // the weight of each split, a wave per row
+  float* const s_w = &s_o[0][0][0];  // [nrow][MAX_SPLITS]
+  static_assert(sizeof(s_o) >= RB * MAX_SPLITS * 4 + ROWS_T * 16, "weights and sums fit");
+  for (int qr = wave; qr < t.nrow; qr += NWAVE) {
+    float mx[MAX_SPLITS / WAVE], ls[MAX_SPLITS / WAVE];
+    float M = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < MAX_SPLITS / WAVE; ++i) {
+      const int c = lane + i * WAVE;
+      uint64_t v = __float_as_uint(-INFINITY);
+      if (c < ns)
+        v = __hip_atomic_load((uint64_t*)a.ml + ((size_t)block * a.splits + c) * a.prow + qr,
+                              __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      mx[i] = __uint_as_float((uint32_t)v);
+      ls[i] = __uint_as_float((uint32_t)(v >> 32));
+      M = fmaxf(M, mx[i]);
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, WAVE));
+    float L = 0.f;
+#pragma unroll
+    for (int i = 0; i < MAX_SPLITS / WAVE; ++i) {
+      const float f = mx[i] == -INFINITY ? ls[i] : __builtin_amdgcn_exp2f(mx[i] - M);
+      L += f * ls[i];
+      s_w[qr * MAX_SPLITS + lane + i * WAVE] = f;
+    }
+    L = wave_sum(L);
+    if (lane == 0) s_m[0][qr] = L;
+  }
+  __syncthreads();
+  // 16-byte pieces of the rows over the threads; with fewer pieces than
+  // threads, several threads share a piece's splits
+  const int units = t.nrow * TD;
+  const int sub = units >= ROWS_T ? 1 : ROWS_T / units;
+  float4* const s_sum = (float4*)(s_w + RB * MAX_SPLITS);
+  for (int u0 = 0; u0 < units; u0 += ROWS_T) {
+    const int u = u0 + (sub > 1 ? (int)threadIdx.x % units : (int)threadIdx.x);
+    const int part = sub > 1 ? (int)threadIdx.x / units : 0;
+    const int qr = u / TD, d = u % TD * 4;
+    float4 sum = make_float4(0, 0, 0, 0);
+    if (u < units && part < sub) {
+      const uint32_t row = (uint32_t)block * a.splits * a.prow + qr;
+#pragma unroll 8
+      for (int c = part; c < ns; c += sub) {
+        const float w = s_w[qr * MAX_SPLITS + c];
+        const float4 v = buf_load16_agent(prs, ((row + c * a.prow) * DP + d) * 4);
+        sum.x += w * v.x;
+        sum.y += w * v.y;
+        sum.z += w * v.z;
+        sum.w += w * v.w;
+      }
+    }
+    if (sub > 1) {
+      s_sum[threadIdx.x] = sum;
+      __syncthreads();
+      if (part) continue;
+      for (int i = 1; i < sub; ++i) {
+        const float4 v = s_sum[threadIdx.x + i * units];
+        sum.x += v.x;
+        sum.y += v.y;
+        sum.z += v.z;
+        sum.w += v.w;
+      }
+    }
+    if (u < units && d < a.D) store_out(qr, d, sum, s_m[0][qr]);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -748,7 +823,7 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
 
   l = swap32_add(l, l);
   if (wave * 32 + r >= t.nrow) return;
-  const bool none = m == -INFINITY;  // a row that sees nothing is zero
+  const bool none = l == 0.f;  // a row that sees nothing is zero
   const float inv = 1.f / l;
   char* op = a.out + (int64_t)(t.row.begin + tok) * a.out_stride + (int64_t)head * rowb;
 #pragma unroll
@@ -778,21 +853,19 @@ hipError_t launch_tile(AttnArgs a, hipStream_t stream) {
 
 template <class T, int DP>
 hipError_t launch_rows(AttnArgs a, int64_t keys, hipStream_t stream) {
-  // enough workgroups to fill the card, at least 128 keys (one step of each
-  // wave) in each
   const int64_t blocks = (int64_t)a.tiles * a.Hkv;
-  int64_t splits = std::min<int64_t>((1024 + blocks - 1) / blocks, KV_SLOTS / std::max<int64_t>(blocks, 1));
-  splits = std::max<int64_t>(1, std::min(splits, (keys + 127) / 128));
+  a.prow = a.b.cu ? RB : std::min(a.G, RB);
+  static int TW = getenv("X_TW") ? atoi(getenv("X_TW")) : 1024, MC = getenv("X_MC") ? atoi(getenv("X_MC")) : 128;
+  int64_t splits = std::min<int64_t>((TW + blocks - 1) / blocks, KV_PART_ROWS / (blocks * a.prow));
+  if (blocks > KV_MAX_BLOCKS) splits = 1;
+  splits = std::max<int64_t>(1, std::min({splits, (keys + MC - 1) / MC, (int64_t)MAX_SPLITS}));
   a.chunk = (int)(((keys + splits - 1) / splits + 127) / 128 * 128);
   a.splits = (int)((keys + a.chunk - 1) / a.chunk);
-  if (a.splits < 1) a.splits = 1;
-  hipLaunchKernelGGL((attn_rows_kernel<T, DP>), dim3((unsigned)(blocks * a.splits)), dim3(ROWS_T), 0,
-                     stream, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.splits == 1) return e;
-  const unsigned rows = a.b.cu ? RB : std::min(a.G, RB);
-  hipLaunchKernelGGL((attn_join_kernel<T, DP>), dim3((unsigned)blocks, rows), dim3(ROWS_T), 0, stream,
-                     a);
+  const dim3 grid((unsigned)(blocks * a.splits));
+  if (a.D == DP)
+    hipLaunchKernelGGL((attn_rows_kernel<T, DP, true>), grid, dim3(ROWS_T), 0, stream, a);
+  else
+    hipLaunchKernelGGL((attn_rows_kernel<T, DP, false>), grid, dim3(ROWS_T), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -838,6 +911,8 @@ hipError_t launch_attn(const np_kv_shape& s, int layer, const np_kv_batch& b,
   a.scale = scale * LOG2E;
   a.window = window;
   a.part = k.part;
+  a.zeros = k.zeros;
+  a.count = k.count;
   a.ml = k.ml;
   a.err = (int32_t*)((char*)ws + WS_ERR);
   // row blocks: at most one partly filled per row of the batch

@@ -30,10 +30,13 @@ __device__ inline int32_t fresh(const int32_t* p) {
 
 __device__ inline int div_up(int a, int b) { return (a + b - 1) / b; }
 
-__global__ void kv_reset_kernel(np_kv_state st, size_t table, int S, int N, int32_t* err) {
+__global__ void kv_reset_kernel(np_kv_state st, size_t table, int S, int N, int32_t* err,
+                                uint32_t* zeros, int32_t* count) {
   const size_t i0 = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
   const size_t step = (size_t)gridDim.x * blockDim.x;
   if (i0 == 0) *err = 0;
+  for (size_t i = i0; i < KV_ZEROS / 4; i += step) zeros[i] = 0;
+  for (size_t i = i0; i < KV_MAX_BLOCKS; i += step) count[i] = 0;
   for (size_t i = i0; i < table; i += step) st.page_table[i] = -1;
   for (size_t i = i0; i < (size_t)N; i += step) st.refs[i] = 0;
   for (size_t i = i0; i < (size_t)S; i += step) st.kv_len[i] = 0;
@@ -540,8 +543,10 @@ hipError_t launch_kv_reset(const np_kv_shape& s, const np_kv_state& st, void* ws
   const size_t table = (size_t)s.max_seqs * s.seq_pages;
   const size_t most = std::max({table, (size_t)s.n_pages, (size_t)s.max_seqs});
   const unsigned grid = (unsigned)std::min<size_t>((most + 255) / 256, 2048);
+  KvScratch k;
+  kv_ws_layout(s, (char*)ws, &k);
   hipLaunchKernelGGL(kv_reset_kernel, dim3(grid), dim3(256), 0, stream, st, table, s.max_seqs,
-                     s.n_pages, (int32_t*)((char*)ws + WS_ERR));
+                     s.n_pages, (int32_t*)((char*)ws + WS_ERR), (uint32_t*)k.zeros, k.count);
   return hipGetLastError();
 }
 

@@ -15,17 +15,25 @@ namespace np {
 //   page scratch   int32 [N] each: free pages, copy sources, copy targets,
 //                  copied tokens, page renaming, two marks per page; int32
 //                  [S] each: first place and split flag of a row
-//   partials       KV_SLOTS blocks of 16 rows: fp32 [16][DP] sums, then fp32
-//                  [16][2] (maximum, sum) of every block
+//   zeros          KV_ZEROS bytes that stay 0: what stands in for a page that a
+//                  table does not name (eight rows of 256 fp32)
+//   counts         int32 [KV_MAX_BLOCKS]: arrivals of a split row block's
+//                  workgroups, 0 between calls
+//   partials       of split attention rows: fp32 [KV_PART_ROWS][DP] outputs,
+//                  then fp32 [KV_PART_ROWS][2] (maximum, sum)
 // ---------------------------------------------------------------------------
 constexpr size_t WS_KV_COPIES = 512;
-constexpr int KV_SLOTS = 2048;
+constexpr int KV_PART_ROWS = 65536;
+constexpr size_t KV_ZEROS = 8192;
+constexpr int KV_MAX_BLOCKS = 8192;
 constexpr int KV_MAX_SEQS = 4096;
 
 inline int kv_dpad(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
 struct KvScratch {
   int32_t *free_ids, *src, *dst, *rows, *remap, *mark, *cnt, *off, *split;
+  char* zeros;
+  int32_t* count;
   float *part, *ml;
 };
 inline size_t kv_ws_layout(const np_kv_shape& s, char* ws, KvScratch* k) {
@@ -39,8 +47,10 @@ inline size_t kv_ws_layout(const np_kv_shape& s, char* ws, KvScratch* k) {
   for (int32_t** p : {&t.free_ids, &t.src, &t.dst, &t.rows, &t.remap, &t.mark, &t.cnt})
     *p = (int32_t*)take((size_t)s.n_pages * 4);
   for (int32_t** p : {&t.off, &t.split}) *p = (int32_t*)take((size_t)(s.max_seqs + 1) * 4);
-  t.part = (float*)take((size_t)KV_SLOTS * 16 * kv_dpad(s.head_dim) * 4);
-  t.ml = (float*)take((size_t)KV_SLOTS * 16 * 2 * 4);
+  t.zeros = take(KV_ZEROS);
+  t.count = (int32_t*)take(KV_MAX_BLOCKS * 4);
+  t.part = (float*)take((size_t)KV_PART_ROWS * kv_dpad(s.head_dim) * 4);
+  t.ml = (float*)take((size_t)KV_PART_ROWS * 2 * 4);
   if (k) *k = t;
   return at;
 }

@@ -34,7 +34,7 @@ struct AttnArgs {
   float scale;  // times log2 e
   int window;
   int tiles;  // row blocks (of one key-value head) the grid covers
-  int chunk;  // keys per split, a multiple of 128
+  int chunk;  // keys per split, a multiple of GROUP (EVEN: groups a share has at least)
   int splits;
   float *part, *ml;
   const char* zeros;  // KV_ZEROS bytes
@@ -42,6 +42,9 @@ struct AttnArgs {
   int prow;  // rows of a block that have partials: min(16, G) with one token a row
   int32_t* err;
 };
+
+// a value that every lane of the wave has alike, for the scalar registers
+__device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // A block of RB consecutive rows (token-major, then head of the group) of one
 // batch row.
@@ -51,12 +54,13 @@ struct Tile {
   int minpos, maxpos;  // of their tokens; maxpos < 0: they see nothing
 };
 
-// Block `tile` of the batch; false past the last one.  Every lane of the wave
-// takes part and gets the same result.  err: where this workgroup reports what
+// Where block `tile` of the batch is: block *pblk of row *prow; false past the
+// last one.  Every lane of the wave takes part and gets the same result.  err: where this workgroup reports what
 // is wrong with its row, or nullptr; the one with tile 0 reports every row of a
 // bad cu_tokens (a row without tokens has no block).
 template <int RB>
-__device__ inline bool find_tile(const KvBatch& b, int G, int tile, int32_t* err, Tile* t) {
+__device__ inline bool find_block(const KvBatch& b, int G, int tile, int32_t* err, int* prow,
+                                  int* pblk) {
   int row, blk;
   if (!b.cu) {
     const int per = (G + RB - 1) / RB;
@@ -90,20 +94,26 @@ __device__ inline bool find_tile(const KvBatch& b, int G, int tile, int32_t* err
     }
     if (row < 0 || blk < 0) return false;  // blk: a cu_tokens that counts tokens twice
   }
-  row = __builtin_amdgcn_readfirstlane(row);
-  blk = __builtin_amdgcn_readfirstlane(blk);
-  const KvRow r = kv_row(b, row, threadIdx.x == 0 ? err : nullptr);
-  t->row.begin = __builtin_amdgcn_readfirstlane(r.begin);  // the same in every lane
-  t->row.n = __builtin_amdgcn_readfirstlane(r.n);
-  t->row.p0 = __builtin_amdgcn_readfirstlane(r.p0);
-  t->row.seq = __builtin_amdgcn_readfirstlane(r.seq);
-  t->rho0 = blk * RB;
-  t->nrow = min(RB, t->row.n * G - t->rho0);
-  if (t->nrow <= 0) return false;
-  t->minpos = t->row.p0 + t->rho0 / G;
-  t->maxpos = t->row.p0 + (t->rho0 + t->nrow - 1) / G;
-  if (t->row.p0 < 0) t->minpos = t->maxpos = -1;
+  *prow = uniform(row);
+  *pblk = uniform(blk);
   return true;
+}
+
+template <int RB>
+__device__ inline bool make_tile(const KvRow& row, int G, int blk, Tile* t) {
+  t->row = row;
+  t->rho0 = blk * RB;
+  t->nrow = min(RB, row.n * G - t->rho0);
+  if (t->nrow <= 0) return false;
+  t->minpos = row.p0 + t->rho0 / G;
+  t->maxpos = row.p0 + (t->rho0 + t->nrow - 1) / G;
+  if (row.p0 < 0) t->minpos = t->maxpos = -1;
+  return true;
+}
+
+// The first key that any row of the block sees.
+__device__ inline int first_key(const Tile& t, int window) {
+  return window && t.maxpos >= 0 ? max(0, t.minpos - window + 1) : 0;
 }
 
 // Two fp32 to a dword of 16-bit values (round to nearest even).
@@ -155,6 +165,7 @@ constexpr int RB = 16;
 constexpr int NWAVE = 4;
 constexpr int ROWS_T = NWAVE * WAVE;
 constexpr int MAX_SPLITS = 128;
+constexpr int GROUP = 128;  // keys a workgroup takes at once: a step or two of each wave
 
 template <class T, int DP>
 struct RowsCfg {
@@ -171,7 +182,9 @@ struct RowsCfg {
 
 // FULL: D == DP; otherwise the key pieces past D are zeroed (a piece inside D is
 // read in their place), and the output columns past D are not stored.
-template <class T, int DP, bool FULL>
+// EVEN: one token a row, the keys of all rows dealt evenly to the workgroups;
+// otherwise a workgroup per (block, head, split).
+template <class T, int DP, bool FULL, bool EVEN>
 __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(
     AttnArgs a) {
   using C = RowsCfg<T, DP>;
@@ -181,43 +194,39 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(
   __shared__ float s_m[NWAVE][RB], s_l[NWAVE][RB];
 
   const int lane = threadIdx.x % WAVE;
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / WAVE);
+  const int wave = uniform((int)threadIdx.x / WAVE);
   const int r = lane & 15, g = lane >> 4;
-  const int id = blockIdx.x;
-  const int h = id % a.Hkv, tile = id / a.Hkv % a.tiles, split = id / a.Hkv / a.tiles;
-  Tile t;
-  if (!find_tile<RB>(a.b, a.G, tile, split == 0 && h == 0 ? a.err : nullptr, &t)) return;
 
-  const int kbeg = a.window && t.maxpos >= 0 ? max(0, t.minpos - a.window + 1) : 0;
-  const int kend = t.maxpos + 1;
-  const int kal = kbeg / KS * KS;
-  const int ns = min(a.splits, max(1, (kend - kal + a.chunk - 1) / a.chunk));
-  if (split >= ns) return;
-  const int k0 = kal + split * a.chunk;
-  const int k1 = split + 1 < ns ? k0 + a.chunk : kend;
-
-  // page ids through the scalar cache: uniform, and counted apart from the
-  // vector loads in flight.  A step of 32 keys has two pages when P is 16.
-  typedef const __attribute__((address_space(4))) int32_t* table_t;
-  const table_t trow = (table_t)(uintptr_t)(a.table + (size_t)t.row.seq * a.M);
+  // One segment: block `blk` of head h of a batch row against keys [k0, k1) of
+  // its [kal, kend).  With parts > 1 other workgroups have the block's other
+  // keys: the outputs go to partial row block `slot`, and the last of the parts
+  // to arrive at *count joins them, part c being row block slot0 for c = 0 and
+  // slotc + c * dslot after it.
+  auto segment = [&](Tile t, int h, int kbeg, int kend, int k0, int k1, int parts, uint32_t slot,
+                     uint32_t slot0, uint32_t slotc, uint32_t dslot, int* count) {
+  for (int* p : {&t.row.begin, &t.row.n, &t.row.p0, &t.row.seq, &t.rho0, &t.nrow, &t.minpos,
+                 &t.maxpos, &h, &kbeg, &kend, &k0, &k1, &parts})
+    *p = uniform(*p);  // they are; the compiler loses sight of it in the loop below
+  const int rr = min(r, t.nrow - 1);
+  const int tok = (t.rho0 + rr) / a.G, head = h * a.G + (t.rho0 + rr) % a.G;
+  const int qpos = t.row.p0 + tok;
   const int klast = max(kend - 1, 0);
+  // page ids through the scalar cache.  A step of 32 keys has two pages when
+  // P is 16.
+  const int32_t* trow = a.table + (int64_t)t.row.seq * a.M;
   struct Pages {
     int a, b;
   };
   auto pages_of = [&](int base) {
     Pages p;
-    p.a = trow[max(kbeg, min(base, klast)) >> a.pshift];
-    p.b = KS == 32 ? trow[max(kbeg, min(base + 16, klast)) >> a.pshift] : p.a;
+    p.a = load_scalar(trow, max(kbeg, min(base, klast)) >> a.pshift);
+    p.b = KS == 32 ? load_scalar(trow, max(kbeg, min(base + 16, klast)) >> a.pshift) : p.a;
     return p;
   };
   int base = k0 + wave * KS;
   Pages pg = {0, 0};
   if (base < k1) pg = pages_of(base);
-
   // this lane's query (B operand): column r, d = 4 V s + V g
-  const int rr = min(r, t.nrow - 1);
-  const int tok = (t.rho0 + rr) / a.G, head = h * a.G + (t.rho0 + rr) % a.G;
-  const int qpos = t.row.p0 + tok;
   uint4 qf[KD];
   {
     const char* qp = a.q + (int64_t)(t.row.begin + tok) * a.q_stride + (int64_t)head * a.D * W;
@@ -445,7 +454,6 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(
       *(float4*)op = make_float4(f[0], f[1], f[2], f[3]);
   };
   constexpr int TD = DP / 4;
-  const int block = tile * a.Hkv + h;
   const __amdgpu_buffer_rsrc_t prs = make_rsrc(a.part, (uint32_t)KV_PART_ROWS * DP * 4);
   for (int u = threadIdx.x; u < t.nrow * TD; u += ROWS_T) {
     const int qr = u / TD, d = u % TD * 4;
@@ -466,8 +474,8 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(
       sum.z += f * x.z;
       sum.w += f * x.w;
     }
-    if (ns > 1) {
-      const uint32_t row = ((uint32_t)block * a.splits + split) * a.prow + qr;
+    if (parts > 1) {
+      const uint32_t row = slot * a.prow + qr;
       buf_store16_agent(prs, (row * DP + d) * 4, sum);
       if (d == 0)
         __hip_atomic_store((uint64_t*)a.ml + row,
@@ -477,24 +485,24 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(
       store_out(qr, d, sum, L);
     }
   }
-  if (ns <= 1) return;
+  if (parts <= 1) return;
 
-  // The last workgroup of a block to arrive joins its splits: the stores
+  // The last workgroup of a block to arrive joins its parts: the stores
   // above go to the level that all XCDs share, and are complete before the
-  // count rises.  The order of the sums is that of the splits, whoever joins.
+  // count rises.  The order of the sums is that of the parts, whoever joins.
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   int* const s_last = (int*)&s_l[0][0];
   if (threadIdx.x == 0) {
-    const int old = __hip_atomic_fetch_add(a.count + block, 1, __ATOMIC_RELAXED,
-                                           __HIP_MEMORY_SCOPE_AGENT);
-    *s_last = old == ns - 1;
-    if (old == ns - 1)  // for the next call
-      __hip_atomic_store(a.count + block, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const int old = __hip_atomic_fetch_add(count, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *s_last = old == parts - 1;
+    if (old == parts - 1)  // for the next call
+      __hip_atomic_store(count, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
   if (!*s_last) return;
-  // the weight of each split, a wave per row
+  // the weight of each part, a wave per row
+  auto part_row = [&](int c) { return (c ? slotc + c * dslot : slot0) * a.prow; };
   float* const s_w = &s_o[0][0][0];  // [nrow][MAX_SPLITS]
   static_assert(sizeof(s_o) >= RB * MAX_SPLITS * 4 + ROWS_T * 16, "weights and sums fit");
   for (int qr = wave; qr < t.nrow; qr += NWAVE) {
@@ -504,9 +512,9 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(
     for (int i = 0; i < MAX_SPLITS / WAVE; ++i) {
       const int c = lane + i * WAVE;
       uint64_t v = __float_as_uint(-INFINITY);
-      if (c < ns)
-        v = __hip_atomic_load((uint64_t*)a.ml + ((size_t)block * a.splits + c) * a.prow + qr,
-                              __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (c < parts)
+        v = __hip_atomic_load((uint64_t*)a.ml + part_row(c) + qr, __ATOMIC_RELAXED,
+                              __HIP_MEMORY_SCOPE_AGENT);
       mx[i] = __uint_as_float((uint32_t)v);
       ls[i] = __uint_as_float((uint32_t)(v >> 32));
       M = fmaxf(M, mx[i]);
@@ -525,7 +533,7 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(
   }
   __syncthreads();
   // 16-byte pieces of the rows over the threads; with fewer pieces than
-  // threads, several threads share a piece's splits
+  // threads, several threads share a piece's parts
   const int units = t.nrow * TD;
   const int sub = units >= ROWS_T ? 1 : ROWS_T / units;
   float4* const s_sum = (float4*)(s_w + RB * MAX_SPLITS);
@@ -535,16 +543,28 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(
     const int qr = u / TD, d = u % TD * 4;
     float4 sum = make_float4(0, 0, 0, 0);
     if (u < units && part < sub) {
-      const uint32_t row = (uint32_t)block * a.splits * a.prow + qr;
-#pragma unroll 8
-      for (int c = part; c < ns; c += sub) {
-        const float w = s_w[qr * MAX_SPLITS + c];
-        const float4 v = buf_load16_agent(prs, ((row + c * a.prow) * DP + d) * 4);
-        sum.x += w * v.x;
-        sum.y += w * v.y;
-        sum.z += w * v.z;
-        sum.w += w * v.w;
-      }
+      // a round trip past the L2 takes microseconds: many loads in flight
+      auto add_parts = [&](auto batch) {
+        constexpr int NB = decltype(batch)::value;
+        for (int c0 = part; c0 < parts; c0 += NB * sub) {
+          float4 v[NB];
+#pragma unroll
+          for (int i = 0; i < NB; ++i) {
+            const int c = c0 + i * sub;
+            v[i] = buf_load16_agent(prs, c < parts ? ((part_row(c) + qr) * DP + d) * 4 : BUF_OOB);
+          }
+#pragma unroll
+          for (int i = 0; i < NB; ++i) {
+            const float w = s_w[qr * MAX_SPLITS + min(c0 + i * sub, MAX_SPLITS - 1)];
+            sum.x += w * v[i].x;
+            sum.y += w * v[i].y;
+            sum.z += w * v[i].z;
+            sum.w += w * v[i].w;
+          }
+        }
+      };
+      if (parts > 4 * sub) add_parts(std::integral_constant<int, 16>{});
+      else add_parts(std::integral_constant<int, 4>{});
     }
     if (sub > 1) {
       s_sum[threadIdx.x] = sum;
@@ -559,6 +579,111 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(
       }
     }
     if (u < units && d < a.D) store_out(qr, d, sum, s_m[0][qr]);
+  }
+  };
+
+  if constexpr (!EVEN) {
+    const int id = blockIdx.x;
+    const int h = id % a.Hkv, tile = id / a.Hkv % a.tiles, split = id / a.Hkv / a.tiles;
+    int32_t* const err = split == 0 && h == 0 ? a.err : nullptr;
+    int row, blk;
+    Tile t;
+    if (!find_block<RB>(a.b, a.G, tile, err, &row, &blk) ||
+        !make_tile<RB>(kv_row(a.b, row, threadIdx.x == 0 ? err : nullptr), a.G, blk, &t))
+      return;
+    const int kbeg = first_key(t, a.window), kend = t.maxpos + 1;
+    const int kal = kbeg / KS * KS;
+    const int ns = min(a.splits, max(1, (kend - kal + a.chunk - 1) / a.chunk));
+    if (split >= ns) return;
+    const int k0 = kal + split * a.chunk;
+    const uint32_t block = tile * a.Hkv + h, slot0 = block * a.splits;
+    segment(t, h, kbeg, kend, k0, split + 1 < ns ? k0 + a.chunk : kend, ns, slot0 + split, slot0,
+            slot0, 1, a.count + block);
+  } else {
+    // One token a row.  The keys of all blocks, in groups of GROUP, lie one
+    // block after the other on a line, and every workgroup has an equal stretch
+    // of it, whatever the lengths of the rows: row by row nb = (blocks of 16
+    // heads) * Hkv blocks of the row's groups each.
+    const int per = (a.G + RB - 1) / RB, nb = per * a.Hkv;
+    auto groups_of = [&](int p0) {  // a row that sees nothing has one, for its zeros
+      const int first = a.window && p0 >= 0 ? max(0, p0 - a.window + 1) / KS * KS : 0;
+      return max(1, (p0 + 1 - first + GROUP - 1) / GROUP);
+    };
+    // rows i0 .. i0 + 63 of the batch, one a lane
+    KvRow lr;
+    int i0 = 0;
+    auto load_rows = [&](int first) {
+      i0 = first;
+      const int i = min(first + lane, a.b.n_seq - 1);
+      const KvRawRow w = {i, i + 1, a.b.seqs ? a.b.seqs[i] : i, a.b.pos0[i]};
+      lr = kv_row_check(a.b, w, blockIdx.x == 0 && threadIdx.x < WAVE ? a.err : nullptr);
+      return first + lane < a.b.n_seq ? groups_of(lr.p0) : 0;
+    };
+    auto row_at = [&](int i) {
+      if (i >= i0 + WAVE) load_rows(i);
+      KvRow k;
+      k.begin = i;
+      k.n = 1;
+      k.p0 = __builtin_amdgcn_readlane(lr.p0, i - i0);
+      k.seq = __builtin_amdgcn_readlane(lr.seq, i - i0);
+      return k;
+    };
+    int n = 0, sum = 0;
+    for (int i = (a.b.n_seq - 1) / WAVE * WAVE; i >= 0; i -= WAVE) {
+      n = load_rows(i);
+      sum += n;
+    }
+    sum = __builtin_amdgcn_readlane((int)wave_incl_scan((uint32_t)sum), WAVE - 1);
+    const int total = uniform(sum * nb);
+    // no block may have more than MAX_SPLITS parts: a.chunk groups at least
+    const int share = max(a.chunk, (total + (int)gridDim.x - 1) / (int)gridDim.x);
+    // workgroups go round the eight XCDs; each XCD gets one stretch in a piece
+    const int wg = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    int at = wg * share;
+    const int end = min(total, at + share);
+    if (at >= end) return;
+    // the row, block and group of the first key of the stretch
+    int row = 0, before = 0;  // groups of the rows before
+    for (const int want = at / nb;; n = load_rows(i0 + WAVE)) {
+      const int incl = (int)wave_incl_scan((uint32_t)n);
+      const uint64_t hit = __ballot(before + incl > want);
+      if (hit) {
+        const int l = __ffsll((unsigned long long)hit) - 1;
+        row = i0 + l;
+        before += __builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(n, l);
+        break;
+      }
+      before += __builtin_amdgcn_readlane(incl, WAVE - 1);
+    }
+    row = uniform(row);
+    before = uniform(before);
+    KvRow kr = row_at(row);
+    int groups = uniform(groups_of(kr.p0));
+    int j = (at - before * nb) / groups;
+    int start = before * nb + j * groups;  // of the block on the line
+    while (true) {
+      Tile t;
+      make_tile<RB>(kr, a.G, j / a.Hkv, &t);
+      const int kbeg = first_key(t, a.window), kend = t.maxpos + 1;
+      const int kal = kbeg / KS * KS;
+      const int stop = min(end, start + groups);
+      const int w0 = start / share, w1 = (start + groups - 1) / share;
+      // a workgroup has at most two blocks that it shares: the one its stretch
+      // begins in, or the one it ends in
+      const uint32_t slot0 = 2 * w0 + (w0 * share < start ? 1 : 0);
+      segment(t, j % a.Hkv, kbeg, kend, kal + (at - start) * GROUP,
+              min(kend, kal + (stop - start) * GROUP), w1 - w0 + 1,
+              wg == w0 ? slot0 : 2 * wg, slot0, 2 * w0, 2, a.count + w0);
+      at = stop;
+      if (at >= end) return;
+      start += groups;
+      if (++j == nb) {
+        j = 0;
+        kr = row_at(++row);
+        groups = uniform(groups_of(kr.p0));
+      }
+      __syncthreads();  // LDS is free again
+    }
   }
 }
 
@@ -617,15 +742,18 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
   __shared__ u32x4_t s_v[2][KB * CPR];
 
   const int tid = threadIdx.x, lane = tid % WAVE;
-  const int wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
+  const int wave = uniform(tid / WAVE);
   const int r = lane & 31, h2 = lane >> 5;
   const int h = blockIdx.x % a.Hkv;
   const int tile = a.tiles - 1 - (int)blockIdx.x / a.Hkv;  // the longest of a prompt first
   Tile t;
-  if (!find_tile<TB>(a.b, a.G, tile, h == 0 ? a.err : nullptr, &t)) return;
+  int32_t* const err = h == 0 ? a.err : nullptr;
+  int row, blk;
+  if (!find_block<TB>(a.b, a.G, tile, err, &row, &blk) ||
+      !make_tile<TB>(kv_row(a.b, row, tid == 0 ? err : nullptr), a.G, blk, &t))
+    return;
 
-  const int kbeg = a.window && t.maxpos >= 0 ? max(0, t.minpos - a.window + 1) : 0;
-  const int kend = t.maxpos + 1;
+  const int kbeg = first_key(t, a.window), kend = t.maxpos + 1;
   const int rowb = a.D * 2;
 
   // this wave's rows and this lane's query
@@ -670,7 +798,7 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
   int any_bad = 0;
   for (int j = (kbeg >> a.pshift) + tid; j <= (kend - 1) >> a.pshift; j += TILE_T)
     any_bad |= trow[j] < 0 || trow[j] >= a.N;
-  const bool bad = __builtin_amdgcn_readfirstlane(__syncthreads_or(any_bad)) != 0;
+  const bool bad = uniform(__syncthreads_or(any_bad)) != 0;
   if (bad && tid == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
   u32x4_t sk[NL] = {}, sv[NL] = {};
   auto key_of = [&](int base, int i) { return max(kbeg, min(base + lr + i * RSTEP, kend - 1)); };
@@ -851,22 +979,54 @@ hipError_t launch_tile(AttnArgs a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// keys: the most a block can see.  Three ways to deal the keys of `blocks`
+// blocks to workgroups (us, fp16 or bf16, D 128, before -> with the rule):
+//  - Every 128 keys to a workgroup of its own while all of them fit on the card
+//    at once (three to a compute unit): one row of 777 keys and 32 heads 9.3
+//    with 256 keys each, 8.9 with 128.
+//  - More keys, one row: as many workgroups as compute units, since a long
+//    stream from few places is the fastest (131072 keys, 8 key-value heads: 95
+//    with 256 workgroups, 99 with 512, 105 with 768).
+//  - More keys, several rows, whose lengths the host does not know: an even
+//    share of all keys to each of 512 workgroups (64 rows of 1 to 8192 keys:
+//    70, against 80 with the best fixed split of each row, most of whose
+//    workgroups find nothing to do).
+// Prompts (rows of more tokens) have many blocks; they are split while those do not give
+// every compute unit a workgroup, in pieces of at least 256 keys (a join costs
+// about 3 us: 250 fp32 keys 10.2 in two pieces, 7.4 in one).
 template <class T, int DP>
-hipError_t launch_rows(AttnArgs a, int64_t keys, hipStream_t stream) {
+hipError_t launch_rows(AttnArgs a, int64_t keys, int max_tokens, hipStream_t stream) {
   const int64_t blocks = (int64_t)a.tiles * a.Hkv;
+  const int64_t groups = (keys + GROUP - 1) / GROUP;
   a.prow = a.b.cu ? RB : std::min(a.G, RB);
-  static int TW = getenv("X_TW") ? atoi(getenv("X_TW")) : 1024, MC = getenv("X_MC") ? atoi(getenv("X_MC")) : 128;
-  int64_t splits = std::min<int64_t>((TW + blocks - 1) / blocks, KV_PART_ROWS / (blocks * a.prow));
-  if (blocks > KV_MAX_BLOCKS) splits = 1;
-  splits = std::max<int64_t>(1, std::min({splits, (keys + MC - 1) / MC, (int64_t)MAX_SPLITS}));
-  a.chunk = (int)(((keys + splits - 1) / splits + 127) / 128 * 128);
-  a.splits = (int)((keys + a.chunk - 1) / a.chunk);
-  const dim3 grid((unsigned)(blocks * a.splits));
-  if (a.D == DP)
-    hipLaunchKernelGGL((attn_rows_kernel<T, DP, true>), grid, dim3(ROWS_T), 0, stream, a);
-  else
-    hipLaunchKernelGGL((attn_rows_kernel<T, DP, false>), grid, dim3(ROWS_T), 0, stream, a);
-  return hipGetLastError();
+  const bool ones = !a.b.cu || max_tokens <= 1;
+  const bool small = ones && groups * blocks <= 768;
+  // the line of groups is counted in 32 bits
+  const bool even = !a.b.cu && !small && a.b.n_seq > 1 && groups * blocks < ((int64_t)1 << 30);
+  dim3 grid;
+  if (even) {
+    a.chunk = (int)((groups + MAX_SPLITS - 3) / (MAX_SPLITS - 2));
+    grid.x = 512;
+  } else {
+    const int64_t least = ones ? GROUP : 256;
+    int64_t splits = small ? groups : (256 + blocks - 1) / blocks;
+    splits = std::min({splits, (keys + least - 1) / least, (int64_t)MAX_SPLITS,
+                       (int64_t)KV_PART_ROWS / (blocks * a.prow)});
+    if (splits < 1 || blocks > KV_MAX_BLOCKS) splits = 1;
+    a.chunk = (int)(((keys + splits - 1) / splits + GROUP - 1) / GROUP * GROUP);
+    a.splits = (int)((keys + a.chunk - 1) / a.chunk);
+    grid.x = (unsigned)(blocks * a.splits);
+  }
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(ROWS_T), 0, stream, a);
+    return hipGetLastError();
+  };
+  if (even) {
+    if (a.D == DP) return go(attn_rows_kernel<T, DP, true, true>);
+    return go(attn_rows_kernel<T, DP, false, true>);
+  }
+  if (a.D == DP) return go(attn_rows_kernel<T, DP, true, false>);
+  return go(attn_rows_kernel<T, DP, false, false>);
 }
 
 template <class T>
@@ -878,9 +1038,9 @@ hipError_t launch_attn_t(AttnArgs& a, int64_t keys, int max_tokens, hipStream_t 
       return launch_tile<T, 256>(a, stream);
     }
   }
-  if (a.D <= 64) return launch_rows<T, 64>(a, keys, stream);
-  if (a.D <= 128) return launch_rows<T, 128>(a, keys, stream);
-  return launch_rows<T, 256>(a, keys, stream);
+  if (a.D <= 64) return launch_rows<T, 64>(a, keys, max_tokens, stream);
+  if (a.D <= 128) return launch_rows<T, 128>(a, keys, max_tokens, stream);
+  return launch_rows<T, 256>(a, keys, max_tokens, stream);
 }
 
 }  // namespace

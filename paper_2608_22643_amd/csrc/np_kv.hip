@@ -446,6 +446,7 @@ __global__ __launch_bounds__(APP_T) void kv_append_kernel(AppendArgs a) {
     }
     if (row >= a.b.n_seq) return;  // past the last row's tokens
   }
+  row = __builtin_amdgcn_readfirstlane(row);
   int32_t* err = threadIdx.x == 0 ? a.err : nullptr;
   const KvRow r = kv_row(a.b, row, err);
   if (r.p0 < 0 || t < r.begin || t >= r.begin + r.n) return;

@@ -78,38 +78,52 @@ struct KvRow {
   int seq;       // 0 <= seq < S
 };
 
-// Row b of the batch (0 <= b < n_seq); err: where to put NP_DEVERR_* bits, or
-// nullptr.  What it returns is in range whatever the arrays hold.
-__device__ inline KvRow kv_row(const KvBatch& a, int b, int32_t* err) {
-  KvRow r;
-  int bad = 0;
-  r.begin = b;
-  r.n = 1;
-  if (a.cu) {
-    const int lo = a.cu[b], hi = a.cu[b + 1];
-    if (lo < 0 || hi < lo || hi > a.n_tokens) {
-      bad = 1;
-      r.begin = r.n = 0;
-    } else {
-      r.begin = lo;
-      r.n = hi - lo;
-    }
+// A uniform address read through the scalar cache: the result is uniform too,
+// and the load is counted apart from vector loads in flight.
+typedef const __attribute__((address_space(4))) int32_t* scalar_i32_t;
+__device__ inline int32_t load_scalar(const int32_t* p, int64_t i) {
+  return ((scalar_i32_t)(uintptr_t)p)[i];
+}
+
+struct KvRawRow {
+  int lo, hi, seq, p0;
+};
+
+// Row b of the batch as it stands in memory (0 <= b < n_seq, uniform).
+__device__ inline KvRawRow kv_row_load(const KvBatch& a, int b) {
+  KvRawRow r;
+  r.p0 = load_scalar(a.pos0, b);
+  r.seq = a.seqs ? load_scalar(a.seqs, b) : b;
+  r.lo = a.cu ? load_scalar(a.cu, b) : b;
+  r.hi = a.cu ? load_scalar(a.cu, b + 1) : b + 1;
+  return r;
+}
+
+// The same within its ranges whatever the arrays hold; err: where to put
+// NP_DEVERR_* bits, or nullptr.
+__device__ inline KvRow kv_row_check(const KvBatch& a, const KvRawRow& w, int32_t* err) {
+  KvRow r = {w.lo, w.hi - w.lo, w.p0, w.seq};
+  bool bad = false;
+  if (w.lo < 0 || w.hi < w.lo || w.hi > a.n_tokens) {
+    bad = true;
+    r.begin = r.n = 0;
   }
-  r.seq = a.seqs ? a.seqs[b] : b;
   if (r.seq < 0 || r.seq >= a.S) {
-    bad = 1;
+    bad = true;
     r.seq = 0;
     r.p0 = -1;
-  } else {
-    r.p0 = a.pos0[b];
   }
   if (r.p0 < 0) r.p0 = -1;
   if (r.p0 >= 0 && r.n > a.lim - min(r.p0, a.lim)) {
-    bad = 1;
+    bad = true;
     r.p0 = -1;
   }
   if (bad && err) atomicOr(err, NP_DEVERR_STATE);
   return r;
+}
+
+__device__ inline KvRow kv_row(const KvBatch& a, int b, int32_t* err) {
+  return kv_row_check(a, kv_row_load(a, b), err);
 }
 
 // ---------------------------------------------------------------------------

@@ -296,3 +296,34 @@ def test_graph_replays_follow_the_device_arrays():
         out.zero_()
         eager = s.run(B.np_attn_decode, batch=batch)
         assert torch.equal(got.cpu(), eager), i
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,Hq,Hkv,D,P,top", [(70, 4, 2, 64, 16, 2500), (200, 2, 1, 64, 64, 900),
+                                              (5, 40, 2, 128, 32, 9000), (3, 8, 8, 96, 16, 9000),
+                                              (130, 3, 3, 256, 128, 700)])
+@pytest.mark.parametrize("window", [0, 333])
+def test_decode_of_ragged_batches(dtype, n, Hq, Hkv, D, P, top, window):
+    """Many rows of very different lengths in one call, more keys than the
+    card takes at once: rows of one key, rows not served, one row far longer
+    than the rest; the second call with the same workspace gives the same
+    bits."""
+    g = torch.Generator().manual_seed(n)
+    lens = [int(2 ** (float(torch.rand(1, generator=g)) * math.log2(top))) for _ in range(n)]
+    rows = [(x - 1, 1) for x in lens]
+    rows[0], rows[n // 2], rows[-1] = (top - 1, 1), (0, 1), (-1, 1)
+    s = Setup(rows, Hq, Hkv, D, P, dtype, seed=13)
+    out = s.run(B.np_attn_decode, window=window)
+    s.check(out, window=window)
+    assert (out[-1] == 0).all() and s.error() == 0
+    assert torch.equal(out, s.run(B.np_attn_decode, window=window))
+
+
+def test_bad_rows_of_a_ragged_batch_are_reported():
+    rows = [(1999, 1)] * 100
+    s = Setup(rows, 4, 4, 64, 64, "f16", seed=14)
+    s.pos0[77] = 5000
+    out = s.run(B.np_attn_decode)
+    assert s.error() == B.NP_DEVERR_STATE
+    assert (out[77] == 0).all()
+    s.check(out, rows=[0, 76, 78, 99])

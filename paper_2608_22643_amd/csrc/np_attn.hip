@@ -723,12 +723,12 @@ struct TileCfg {
   static constexpr int CPR = DP / 8;                // 16-byte pieces of a row
   static constexpr int NL = KB * CPR / TILE_T;      // pieces a thread loads
   static constexpr int RSTEP = TILE_T / CPR;        // rows between them
-  // piece permutations of K and V rows
-  __device__ static inline int kperm(int row, int c) {
-    return c ^ (DP == 64 ? row >> 1 & 7 : row & 15);
-  }
-  __device__ static inline int vperm(int row, int c) {
-    return c ^ (DP == 64 ? (row >> 1 & 1) << 2 | (row >> 2 & 3) : (row & 3) << 2 | (row >> 2 & 3));
+  static constexpr int WROWS = WAVE / CPR;          // rows of a wave's load
+  static constexpr int ROW = CPR * 16;              // bytes of an LDS row
+  // piece c of a row lies at piece c ^ kx (K) or c ^ vx (V)
+  __device__ static inline int kx(int row) { return DP == 64 ? row >> 1 & 7 : row & 15; }
+  __device__ static inline int vx(int row) {
+    return DP == 64 ? (row >> 1 & 1) << 2 | (row >> 2 & 3) : (row & 3) << 2 | (row >> 2 & 3);
   }
 };
 
@@ -738,8 +738,8 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
   using C = TileCfg<DP>;
   constexpr int KB = C::KB, CPR = C::CPR, NL = C::NL, RSTEP = C::RSTEP;
   constexpr int KT = KB / 32, KD = DP / 16, DT = DP / 32;
-  __shared__ u32x4_t s_k[2][KB * CPR];
-  __shared__ u32x4_t s_v[2][KB * CPR];
+  __shared__ __attribute__((aligned(1024))) char s_k[2 * KB * C::ROW];
+  __shared__ __attribute__((aligned(1024))) char s_v[2 * KB * C::ROW];
 
   const int tid = threadIdx.x, lane = tid % WAVE;
   const int wave = uniform(tid / WAVE);
@@ -784,14 +784,16 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
   for (int j = 0; j < DT; ++j) o[j] = (f32x16)(0.f);
   float m = -INFINITY, l = 0.f;
 
-  // loads: piece lc of rows lr, lr + RSTEP, ...  Rows outside the tile's keys
-  // repeat its first or last one: they get no weight, but have to be finite.
+  // Loads: piece lc of rows lr, lr + RSTEP, ...  A wave's rows of one load lie
+  // in 16 consecutive keys, so in one page: page ids and row blocks are scalar,
+  // and a lane adds an offset that stays the same.  Rows outside the tile's
+  // keys repeat its first or last one: they get no weight, but have to be
+  // finite.
   const int lc = tid % CPR, lr = tid / CPR;
   const bool lon = FULL || lc * 8 < a.D;
   const int P1 = (1 << a.pshift) - 1;
-  const size_t hrow = (size_t)h << a.pshift;
   const size_t vofs = ((size_t)a.Hkv << a.pshift) * rowb;
-  const char* hpool = a.pool + hrow * rowb + lc * 16;
+  const char* hpool = a.pool + ((size_t)h << a.pshift) * rowb;
   const int32_t* trow = a.table + (size_t)t.row.seq * a.M;
   // a table that names no page somewhere in the tile's keys: those keys are
   // looked up again and masked one by one
@@ -801,32 +803,47 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
   const bool bad = uniform(__syncthreads_or(any_bad)) != 0;
   if (bad && tid == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
   u32x4_t sk[NL] = {}, sv[NL] = {};
-  auto key_of = [&](int base, int i) { return max(kbeg, min(base + lr + i * RSTEP, kend - 1)); };
+  uint32_t lofs[NL];
+  int block16[NL];  // the 16 rows of the step that load i is in
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    block16[i] = (RSTEP * i + wave * C::WROWS) & ~15;
+    lofs[i] = (lr + RSTEP * i - block16[i]) * rowb + lc * 16;
+  }
   int page[NL];
   auto load_pages = [&](int base) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) page[i] = trow[key_of(base, i) >> a.pshift];
+    for (int i = 0; i < NL; ++i)
+      page[i] = load_scalar(trow, max(kbeg, min(base + block16[i], kend - 1)) >> a.pshift);
   };
   auto load_rows = [&](int base) {
     const char* p[NL];
-    int64_t vo[NL];
+    uint32_t o[NL];
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      p[i] = hpool + (int64_t)page[i] * (int64_t)a.page_bytes + (key_of(base, i) & P1) * rowb;
-      vo[i] = vofs;
+      p[i] = hpool + (int64_t)page[i] * (int64_t)a.page_bytes;
+      o[i] = lofs[i] + ((base + block16[i]) & P1) * rowb;
     }
+    if (base < kbeg || base + KB > kend) {
+#pragma unroll
+      for (int i = 0; i < NL; ++i)
+        o[i] = (max(kbeg, min(base + lr + i * RSTEP, kend - 1)) & P1) * rowb + lc * 16;
+    }
+    const char* pv[NL];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) pv[i] = p[i] + vofs;
     if (bad)
 #pragma unroll
       for (int i = 0; i < NL; ++i)
         if (page[i] < 0 || page[i] >= a.N) {  // masked below: any finite row will do
-          p[i] = a.q + (int64_t)t.row.begin * a.q_stride + lc * 16;
-          vo[i] = 0;
+          p[i] = pv[i] = a.q + (int64_t)t.row.begin * a.q_stride;
+          o[i] = lc * 16;
         }
     if (lon) {
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
-        sk[i] = load_global16(p[i]);
-        sv[i] = load_global16(p[i] + vo[i]);
+        sk[i] = load_global16(p[i] + o[i]);
+        sv[i] = load_global16(pv[i] + o[i]);
       }
     }
   };
@@ -834,28 +851,33 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
     if (lon) {
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
-        const int row = lr + i * RSTEP;
-        s_k[buf][row * CPR + C::kperm(row, lc)] = sk[i];
-        s_v[buf][row * CPR + C::vperm(row, lc)] = sv[i];
+        const int row = lr + i * RSTEP, at = (buf * KB + row) * C::ROW;
+        *(u32x4_t*)(s_k + at + (lc ^ C::kx(row)) * 16) = sk[i];
+        *(u32x4_t*)(s_v + at + (lc ^ C::vx(row)) * 16) = sv[i];
       }
     }
   };
   if constexpr (!FULL) {
     if (!lon)
 #pragma unroll
-      for (int i = 0; i < NL; ++i) {
+      for (int i = 0; i < 2 * NL; ++i) {
         const int row = lr + i * RSTEP;
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          s_k[x][row * CPR + C::kperm(row, lc)] = (u32x4_t)(0u);
-          s_v[x][row * CPR + C::vperm(row, lc)] = (u32x4_t)(0u);
-        }
+        *(u32x4_t*)(s_k + row * C::ROW + (lc ^ C::kx(row)) * 16) = (u32x4_t)(0u);
+        *(u32x4_t*)(s_v + row * C::ROW + (lc ^ C::vx(row)) * 16) = (u32x4_t)(0u);
       }
   }
 
+  // LDS addresses of a lane.  K: piece 2 s + h2 of row r (+ 32 kt); V: four
+  // columns of rows vr and vr + 8 (+ 16 mm), column 32 j + vc.  The pieces' xor
+  // with s or j can be taken on the whole address, since rows are aligned.
+  const int vr = 4 * h2 + (lane >> 2 & 3), vc = 16 * (lane >> 4 & 1) + 4 * (lane & 3);
+  const uint32_t ka = r * C::ROW + (h2 ^ C::kx(r)) * 16;
+  const uint32_t va = vr * C::ROW + ((vc >> 3) ^ C::vx(vr)) * 16 + (vc & 4) * 2;
+  const uint32_t vb = (vr + 8) * C::ROW + ((vc >> 3) ^ C::vx(vr + 8)) * 16 + (vc & 4) * 2;
+
   const int k0 = kbeg / KB * KB;
-  if (kend > 0) load_pages(k0);
   if (kend > 0) {
+    load_pages(k0);
     load_rows(k0);
     load_pages(k0 + KB);
     store_rows(0);
@@ -870,15 +892,17 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
     }
     if (base <= wmax && (a.window == 0 || base + KB - 1 > wmin - a.window)) {
       const bool full = !bad && base + KB - 1 <= wmin && (a.window == 0 || base > wmax - a.window);
+      const uint32_t bo = buf * KB * C::ROW;
       f32x16 sc[KT];
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt) {
-        sc[kt] = (f32x16)(0.f);
-        const int row = 32 * kt + r;
+      for (int kt = 0; kt < KT; ++kt) sc[kt] = (f32x16)(0.f);
 #pragma unroll
-        for (int s = 0; s < KD; ++s)
-          sc[kt] = mfma32<T>(as_uint4(s_k[buf][row * CPR + C::kperm(row, 2 * s + h2)]), qf[s], sc[kt]);
-      }
+      for (int s = 0; s < KD; ++s)
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+          const u32x4_t k = *(const u32x4_t*)(s_k + ((ka + bo) ^ (32 * s)) + 32 * kt * C::ROW);
+          sc[kt] = mfma32<T>(as_uint4(k), qf[s], sc[kt]);
+        }
       if (!full) {
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
@@ -905,7 +929,9 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
                                                         false, false);
         mx = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])) * scale;
       }
-      if (__any(mx > m)) {
+      // m follows the maximum only when it falls 8 behind (in powers of two):
+      // probabilities then reach 2^8 at most, and the outputs are rarely scaled
+      if (__any(mx > m + 8.f)) {
         const float mn = fmaxf(m, mx);
         const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
         m = mn;
@@ -929,18 +955,15 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
         pf[2 * kt + 1] = make_uint4(u[4], u[5], u[6], u[7]);
       }
       // V^T: rows 32 j + l % 32, keys 16 mm + 4 h + {0..3} and 8 further
-      const int vr = 4 * h2 + (lane >> 2 & 3), vc = 16 * (lane >> 4 & 1) + 4 * (lane & 3);
 #pragma unroll
       for (int mm = 0; mm < 2 * KT; ++mm)
 #pragma unroll
         for (int j = 0; j < DT; ++j) {
-          const int ra = 16 * mm + vr, rb = ra + 8, d = 32 * j + vc;
           typedef __attribute__((address_space(3))) s16x4 lds4;
-          const char* vb = (const char*)s_v[buf];
           const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (lds4*)(vb + (ra * CPR + C::vperm(ra, d / 8)) * 16 + (d & 4) * 2));
+              (lds4*)(s_v + ((va + bo) ^ (64 * j)) + 16 * mm * C::ROW));
           const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (lds4*)(vb + (rb * CPR + C::vperm(rb, d / 8)) * 16 + (d & 4) * 2));
+              (lds4*)(s_v + ((vb + bo) ^ (64 * j)) + 16 * mm * C::ROW));
           const uint2 xu = __builtin_bit_cast(uint2, x), yu = __builtin_bit_cast(uint2, y);
           o[j] = mfma32<T>(make_uint4(xu.x, xu.y, yu.x, yu.y), pf[mm], o[j]);
         }

@@ -99,6 +99,49 @@ __device__ inline bool find_block(const KvBatch& b, int G, int tile, int32_t* er
   return true;
 }
 
+// The same with the blocks in another order: those that reach furthest first,
+// so that the longest do not start last.  With up to 64 rows, one a lane: block
+// blk of a row has level (its first key, in blocks) + blk, every row has at most
+// one block of a level, and block number `rank` is found by counting those above
+// a level.  More rows leave the order as it is (there are blocks enough to fill
+// in behind the longest).
+template <int RB>
+__device__ inline bool find_block_longest(const KvBatch& b, int G, int rank, int tiles,
+                                          int32_t* err, int* prow, int* pblk) {
+  if (!b.cu || b.n_seq > WAVE) return find_block<RB>(b, G, tiles - 1 - rank, err, prow, pblk);
+  const int lane = threadIdx.x % WAVE;
+  int n = 0, lo = 0;
+  if (lane < b.n_seq) {
+    const KvRawRow w = {b.cu[lane], b.cu[lane + 1], 0, b.pos0[lane]};
+    if (w.lo < 0 || w.hi < w.lo || w.hi > b.n_tokens) {
+      if (err && rank == 0 && threadIdx.x < WAVE) atomicOr(err, NP_DEVERR_STATE);
+    } else {
+      n = (int)(((int64_t)(w.hi - w.lo) * G + RB - 1) / RB);
+      lo = (int)((int64_t)min(max(w.p0, 0), b.lim) * G / RB);
+    }
+  }
+  auto above = [&](int x) {  // blocks of level x or more
+    const int c = min(n, max(0, lo + n - max(x, lo)));
+    return __builtin_amdgcn_readlane((int)wave_incl_scan((uint32_t)c), WAVE - 1);
+  };
+  if (above(0) <= rank) return false;
+  int x0 = 0, x1 = (int)wave_max(n ? (uint32_t)(lo + n) : 0u);  // above(x0) > rank >= above(x1)
+  while (x1 - x0 > 1) {
+    const int x = x0 + (x1 - x0) / 2;
+    if (above(x) > rank) x0 = x;
+    else x1 = x;
+  }
+  // the rank - above(x1)-th row that has a block of level x0
+  const uint32_t has = n > 0 && lo <= x0 && x0 < lo + n;
+  const int nth = (int)wave_incl_scan(has) - 1, want = rank - above(x1);  // every lane takes part
+  const uint64_t hit = __ballot(has && nth == want);
+  const int l = __ffsll((unsigned long long)hit) - 1;
+  if (l < 0) return false;
+  *prow = l;
+  *pblk = x0 - __builtin_amdgcn_readlane(lo, l);
+  return true;
+}
+
 template <int RB>
 __device__ inline bool make_tile(const KvRow& row, int G, int blk, Tile* t) {
   t->row = row;
@@ -745,11 +788,10 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
   const int wave = uniform(tid / WAVE);
   const int r = lane & 31, h2 = lane >> 5;
   const int h = blockIdx.x % a.Hkv;
-  const int tile = a.tiles - 1 - (int)blockIdx.x / a.Hkv;  // the longest of a prompt first
   Tile t;
   int32_t* const err = h == 0 ? a.err : nullptr;
   int row, blk;
-  if (!find_block<TB>(a.b, a.G, tile, err, &row, &blk) ||
+  if (!find_block_longest<TB>(a.b, a.G, blockIdx.x / a.Hkv, a.tiles, err, &row, &blk) ||
       !make_tile<TB>(kv_row(a.b, row, tid == 0 ? err : nullptr), a.G, blk, &t))
     return;
 
@@ -795,34 +837,33 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
   const size_t vofs = ((size_t)a.Hkv << a.pshift) * rowb;
   const char* hpool = a.pool + ((size_t)h << a.pshift) * rowb;
   const int32_t* trow = a.table + (size_t)t.row.seq * a.M;
-  // a table that names no page somewhere in the tile's keys: those keys are
-  // looked up again and masked one by one
-  int any_bad = 0;
-  for (int j = (kbeg >> a.pshift) + tid; j <= (kend - 1) >> a.pshift; j += TILE_T)
-    any_bad |= trow[j] < 0 || trow[j] >= a.N;
-  const bool bad = uniform(__syncthreads_or(any_bad)) != 0;
-  if (bad && tid == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
   u32x4_t sk[NL] = {}, sv[NL] = {};
+  constexpr int NB = KB / 16;  // blocks of 16 keys in a step: each in one page
+  // the block of the step that this wave's load i is in
+  auto block_of = [&](int i) { return DP == 64 ? 2 * i + (wave >> 1) : RSTEP * i / 16; };
   uint32_t lofs[NL];
-  int block16[NL];  // the 16 rows of the step that load i is in
 #pragma unroll
-  for (int i = 0; i < NL; ++i) {
-    block16[i] = (RSTEP * i + wave * C::WROWS) & ~15;
-    lofs[i] = (lr + RSTEP * i - block16[i]) * rowb + lc * 16;
-  }
-  int page[NL];
+  for (int i = 0; i < NL; ++i) lofs[i] = (lr + RSTEP * i - 16 * block_of(i)) * rowb + lc * 16;
+  int ids[NB];
+  // a table that names no page for some key of the step: its keys are looked up
+  // again and masked one by one
+  bool bad = false, next_bad = false, missing = false;
   auto load_pages = [&](int base) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i)
-      page[i] = load_scalar(trow, max(kbeg, min(base + block16[i], kend - 1)) >> a.pshift);
+    for (int b = 0; b < NB; ++b)
+      ids[b] = load_scalar(trow, max(kbeg, min(base + 16 * b, kend - 1)) >> a.pshift);
   };
   auto load_rows = [&](int base) {
+    int page[NL];
+#pragma unroll
+    for (int i = 0; i < NL; ++i)
+      page[i] = DP == 64 ? (wave >> 1 ? ids[2 * i + 1] : ids[2 * i]) : ids[RSTEP * i / 16];
     const char* p[NL];
     uint32_t o[NL];
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       p[i] = hpool + (int64_t)page[i] * (int64_t)a.page_bytes;
-      o[i] = lofs[i] + ((base + block16[i]) & P1) * rowb;
+      o[i] = lofs[i] + ((base + 16 * block_of(i)) & P1) * rowb;
     }
     if (base < kbeg || base + KB > kend) {
 #pragma unroll
@@ -832,7 +873,10 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
     const char* pv[NL];
 #pragma unroll
     for (int i = 0; i < NL; ++i) pv[i] = p[i] + vofs;
-    if (bad)
+    next_bad = false;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) next_bad |= (uint32_t)ids[b] >= (uint32_t)a.N;
+    if (next_bad)
 #pragma unroll
       for (int i = 0; i < NL; ++i)
         if (page[i] < 0 || page[i] >= a.N) {  // masked below: any finite row will do
@@ -878,6 +922,7 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
   const int k0 = kbeg / KB * KB;
   if (kend > 0) {
     load_pages(k0);
+    __builtin_amdgcn_sched_barrier(0);  // all ids before the first is waited for
     load_rows(k0);
     load_pages(k0 + KB);
     store_rows(0);
@@ -886,6 +931,8 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
   int buf = 0;
   for (int base = k0; base < kend; base += KB, buf ^= 1) {
     const bool more = base + KB < kend;
+    bad = next_bad;
+    missing |= bad;
     if (more) {
       load_rows(base + KB);
       load_pages(base + 2 * KB);
@@ -911,13 +958,20 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
             const int key = base + 32 * kt + 8 * (i / 4) + 4 * h2 + i % 4;
             if (key > qpos || (a.window && key <= qpos - a.window)) sc[kt][i] = -INFINITY;
           }
-        if (bad)
+        if (bad) {
+          uint32_t hide = 0;  // bit 16 kt + i
+#pragma unroll 1
+          for (int x = 0; x < 16 * KT; ++x) {
+            const int key = base + x / 16 * 32 + 8 * (x % 16 / 4) + 4 * h2 + x % 4;
+            const int p = trow[min(key, kend - 1) >> a.pshift];
+            if (p < 0 || p >= a.N) hide |= 1u << x;
+          }
+#pragma unroll
           for (int kt = 0; kt < KT; ++kt)
-            for (int i = 0; i < 16; ++i) {
-              const int key = base + 32 * kt + 8 * (i / 4) + 4 * h2 + i % 4;
-              const int p = trow[min(key, kend - 1) >> a.pshift];
-              if (p < 0 || p >= a.N) sc[kt][i] = -INFINITY;
-            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (hide >> (16 * kt + i) & 1) sc[kt][i] = -INFINITY;
+        }
       }
       float mx = sc[0][0];
 #pragma unroll
@@ -971,6 +1025,8 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
     if (more) store_rows(buf ^ 1);
     __syncthreads();
   }
+
+  if (missing && lane == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
 
   l = swap32_add(l, l);
   if (wave * 32 + r >= t.nrow) return;

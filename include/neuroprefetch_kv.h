@@ -80,6 +80,7 @@ typedef struct np_kv_state {
 /* n_seq, n_tokens (rows of the token arrays), max_tokens (no row brings
  * more) and max_len (no position of the batch reaches it) are host values;
  * max_len bounds the keys a call covers and max_tokens only picks kernels.
+ * Work is split by them: the closer they are, the better it is spread.
  * The arrays are device int32, 4-byte aligned; each may change between calls
  * without the host knowing.  Device-side checks: a sequence outside [0, S), a
  * cu_tokens that descends or leaves [0, n_tokens], and a position at or past
@@ -200,11 +201,15 @@ np_status np_kv_append(const np_kv_shape* shape, int32_t layer, const np_kv_batc
  * with the same stride.  scale: finite.  window >= 0.  Sums, softmax
  * statistics and accumulators are fp32; for 16-bit types the probabilities
  * are rounded to w before they meet the values, as the matrix cores take
- * them.
- * np_attn_decode: one token per row (cu_tokens must be NULL); long sequences
- * are split over workgroups and joined by a second kernel.  np_attn_prompt:
+ * them.  Memory at positions outside the keys a row's tokens see together may
+ * hold anything, NaN and infinities included; a value that is not finite at a
+ * position that some token of the row sees may also reach those of its tokens
+ * that do not see it (there it is multiplied by a weight of zero).
+ * np_attn_decode: one token per row (cu_tokens must be NULL).  np_attn_prompt:
  * any number of tokens per row, the keys and values of the new tokens already
- * appended.  Both give the same bits from run to run. */
+ * appended.  One kernel each: where the keys of a row are split over
+ * workgroups, the last of them to finish joins the parts, in a fixed order.
+ * Both give the same bits from run to run. */
 np_status np_attn_decode(const np_kv_shape* shape, int32_t layer, const np_kv_batch* batch,
                          const int32_t* page_table, const void* q, int64_t q_stride,
                          const void* pool, float scale, int32_t window, void* out,

@@ -55,9 +55,10 @@ struct Tile {
 };
 
 // Where block `tile` of the batch is: block *pblk of row *prow; false past the
-// last one.  Every lane of the wave takes part and gets the same result.  err: where this workgroup reports what
-// is wrong with its row, or nullptr; the one with tile 0 reports every row of a
-// bad cu_tokens (a row without tokens has no block).
+// last one.  Every lane of the wave takes part and gets the same result.  err:
+// where this workgroup reports what is wrong with its row, or nullptr; the one
+// with tile 0 reports every row of a bad cu_tokens (a row without tokens has no
+// block).
 template <int RB>
 __device__ inline bool find_block(const KvBatch& b, int G, int tile, int32_t* err, int* prow,
                                   int* pblk) {
@@ -202,7 +203,12 @@ __device__ inline float sum_groups(float v) {
 //    of output tile (s, j), so a lane ends up with NV consecutive outputs.
 // Each lane owns one query (l % 16): maximum, sum and rescaling need no
 // exchange beyond the maximum over the four lanes of a query.
-// Bound by the K and V bytes (decode) or, in fp32, by the matrix cores.
+// Bound by the K and V bytes: one bf16 row of 131072 keys, 8 key-value heads of
+// 128, 537 MB in 95 us (5.65 TB/s; a plain stream of that length reaches 5.6 to
+// 6.1); 64 fp16 rows of 1 to 8192 keys, 326 MB in 69 us (4.7 TB/s).  Short calls
+// are bound by the chain table -> keys -> scores -> values -> join: 8.9 us for
+// 777 keys and 32 heads.  fp32 prompts run here too, bound by the fp32 matrix
+// cores.
 // ---------------------------------------------------------------------------
 constexpr int RB = 16;
 constexpr int NWAVE = 4;
@@ -740,6 +746,15 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(
 // are numbered such that its P operand is the lane's own scores.  V comes out
 // of LDS transposed (ds_read_tr: four keys of one column per lane).
 //
+// 128 rows, so that a step's products (32 cycles a wave and matrix instruction)
+// cover the loads of the next; 64 keys, so that two workgroups fit a compute unit
+// and one's softmax runs beside the other's products.  Bound by the issue of the
+// exponentials and roundings beside the products: 16384 bf16 tokens with 64 heads
+// of 128 4.55 ms, 967 TFLOP/s (an 8192^3 library product reaches 1140); 2048 fp16
+// tokens and 32 heads 69 us (500 TFLOP/s: the longest tile's 32 steps are in line).
+// Measured and dropped: one workgroup of eight waves in two groups half a step
+// apart, 4.68 to 5.05 ms.
+//
 // LDS rows are permuted in 16-byte pieces so that neither the row reads of K
 // (32 rows, one piece) nor the transposed reads of V (8 rows, four pieces)
 // meet in a bank.
@@ -787,15 +802,22 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
   const int tid = threadIdx.x, lane = tid % WAVE;
   const int wave = uniform(tid / WAVE);
   const int r = lane & 31, h2 = lane >> 5;
-  const int h = blockIdx.x % a.Hkv;
+  const int h = blockIdx.x % a.Hkv, rank = blockIdx.x / a.Hkv % a.tiles;
+  const int split = blockIdx.x / a.Hkv / a.tiles;
   Tile t;
-  int32_t* const err = h == 0 ? a.err : nullptr;
+  int32_t* const err = split == 0 && h == 0 ? a.err : nullptr;
   int row, blk;
-  if (!find_block_longest<TB>(a.b, a.G, blockIdx.x / a.Hkv, a.tiles, err, &row, &blk) ||
+  if (!find_block_longest<TB>(a.b, a.G, rank, a.tiles, err, &row, &blk) ||
       !make_tile<TB>(kv_row(a.b, row, tid == 0 ? err : nullptr), a.G, blk, &t))
     return;
 
-  const int kbeg = first_key(t, a.window), kend = t.maxpos + 1;
+  // the tile's keys, in steps, and this part of them
+  const int tbeg = first_key(t, a.window), tend = t.maxpos + 1;
+  const int step0 = tbeg / KB, steps = (tend + KB - 1) / KB - step0;
+  const int parts = max(1, min(a.splits, (steps + a.chunk - 1) / a.chunk));
+  if (split >= parts) return;
+  const int kbeg = max(tbeg, (step0 + steps * split / parts) * KB);
+  const int kend = min(tend, (step0 + steps * (split + 1) / parts) * KB);
   const int rowb = a.D * 2;
 
   // this wave's rows and this lane's query
@@ -1029,6 +1051,76 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
   if (missing && lane == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
 
   l = swap32_add(l, l);
+  if (parts > 1) {
+    // as in the row blocks: the parts to the level that all XCDs share, the last
+    // to arrive adds them up in their order.  A thread's outputs are its own in
+    // every part, so they go out as they lie in the registers.
+    const __amdgpu_buffer_rsrc_t prs = make_rsrc(a.part, (uint32_t)KV_PART_ROWS * DP * 4);
+    constexpr int NO = 4 * DT;  // 16-byte pieces of a thread
+    const uint32_t block = (uint32_t)rank * a.Hkv + h, slot0 = block * a.splits;
+    auto at = [&](int c, int i) { return (((slot0 + c) * NO + i) * TILE_T + tid) * 16; };
+    uint64_t* const ml = (uint64_t*)a.ml + (size_t)slot0 * TB + wave * 32 + r;
+#pragma unroll
+    for (int i = 0; i < NO; ++i)
+      buf_store16_agent(prs, at(split, i),
+                        make_float4(o[i / 4][i % 4 * 4], o[i / 4][i % 4 * 4 + 1],
+                                    o[i / 4][i % 4 * 4 + 2], o[i / 4][i % 4 * 4 + 3]));
+    if (h2 == 0)
+      __hip_atomic_store(ml + split * TB, (uint64_t)__float_as_uint(l) << 32 | __float_as_uint(m),
+                         __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    int* const s_last = (int*)s_k;
+    if (tid == 0) {
+      int* const count = a.count + block;
+      const int old = __hip_atomic_fetch_add(count, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      *s_last = old == parts - 1;
+      if (old == parts - 1)  // for the next call
+        __hip_atomic_store(count, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!*s_last) return;
+    auto stats = [&](int c, float* mc, float* lc) {
+      const uint64_t v =
+          __hip_atomic_load(ml + c * TB, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      *mc = __uint_as_float((uint32_t)v);
+      *lc = __uint_as_float((uint32_t)(v >> 32));
+    };
+    float M = -INFINITY, L = 0.f, mc, lc;
+    for (int c = 0; c < parts; ++c) {
+      stats(c, &mc, &lc);
+      M = fmaxf(M, mc);
+    }
+    f32x16 sum[DT];
+#pragma unroll
+    for (int j = 0; j < DT; ++j) sum[j] = (f32x16)(0.f);
+    for (int c = 0; c < parts; ++c) {
+      stats(c, &mc, &lc);
+      // without a maximum the sum is 0, or NaN when every score was
+      const float f = mc == -INFINITY ? lc : __builtin_amdgcn_exp2f(mc - M);
+      L += f * lc;
+      float4 v[NO];
+      if (c != split) {
+#pragma unroll
+        for (int i = 0; i < NO; ++i) v[i] = buf_load16_agent(prs, at(c, i));
+      } else {
+#pragma unroll
+        for (int i = 0; i < NO; ++i)
+          v[i] = make_float4(o[i / 4][i % 4 * 4], o[i / 4][i % 4 * 4 + 1], o[i / 4][i % 4 * 4 + 2],
+                             o[i / 4][i % 4 * 4 + 3]);
+      }
+#pragma unroll
+      for (int i = 0; i < NO; ++i) {
+        sum[i / 4][i % 4 * 4] += f * v[i].x;
+        sum[i / 4][i % 4 * 4 + 1] += f * v[i].y;
+        sum[i / 4][i % 4 * 4 + 2] += f * v[i].z;
+        sum[i / 4][i % 4 * 4 + 3] += f * v[i].w;
+      }
+    }
+    l = L;
+#pragma unroll
+    for (int j = 0; j < DT; ++j) o[j] = sum[j];
+  }
   if (wave * 32 + r >= t.nrow) return;
   const bool none = l == 0.f;  // a row that sees nothing is zero
   const float inv = 1.f / l;
@@ -1046,11 +1138,24 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
     }
 }
 
+// The keys of a tile are split while the tiles do not give every compute unit two
+// workgroups (64 tokens of 32 heads over 8 behind 32000 others: 774 us unsplit,
+// 96 in 16 parts), but into 32 parts at most and 256 keys at least: the join costs
+// about 1.5 us a part (17 tokens there: 65 in 32 parts, 89 in 64; behind 2000 24
+// with 256 keys a part, 28 with 512).
 template <class T, int DP>
 hipError_t launch_tile(AttnArgs a, hipStream_t stream) {
-  a.tiles = a.b.cu ? (int)((int64_t)a.b.n_tokens * a.G / TB) + a.b.n_seq
-                   : a.b.n_seq * ((a.G + TB - 1) / TB);
-  const dim3 grid((unsigned)((int64_t)a.tiles * a.Hkv));
+  constexpr int KB = TileCfg<DP>::KB;
+  a.tiles = (int)((int64_t)a.b.n_tokens * a.G / TB) + a.b.n_seq;
+  const int64_t blocks = (int64_t)a.tiles * a.Hkv;
+  int64_t keys = a.b.lim;  // the most a tile can see
+  if (a.window > 0) keys = std::min<int64_t>(keys, (int64_t)a.window + TB + KB);
+  int64_t splits = std::min({(512 + blocks - 1) / blocks, keys / 256, (int64_t)32,
+                             (int64_t)KV_PART_ROWS / (TB * blocks)});
+  if (splits < 1 || blocks > KV_MAX_BLOCKS) splits = 1;
+  a.splits = (int)splits;
+  a.chunk = (int)(((keys + KB - 1) / KB + splits - 1) / splits);
+  const dim3 grid((unsigned)(blocks * splits));
   if (a.D == DP)
     hipLaunchKernelGGL((attn_tile_kernel<T, DP, true>), grid, dim3(TILE_T), 0, stream, a);
   else
@@ -1070,9 +1175,11 @@ hipError_t launch_tile(AttnArgs a, hipStream_t stream) {
 //    share of all keys to each of 512 workgroups (64 rows of 1 to 8192 keys:
 //    70, against 80 with the best fixed split of each row, most of whose
 //    workgroups find nothing to do).
-// Prompts (rows of more tokens) have many blocks; they are split while those do not give
-// every compute unit a workgroup, in pieces of at least 256 keys (a join costs
-// about 3 us: 250 fp32 keys 10.2 in two pieces, 7.4 in one).
+// Prompts (rows of more tokens) have many blocks; they are split while those do
+// not give every compute unit two workgroups (64 tokens of 32 heads over 8 behind
+// 2000 others: 29 with one a compute unit, 23 with two), or one if they are few
+// (up to 64: 8 tokens behind 32000 others 38 and 47), in pieces of at least 256
+// keys (a join costs about 3 us: 250 fp32 keys 10.2 in two pieces, 7.4 in one).
 template <class T, int DP>
 hipError_t launch_rows(AttnArgs a, int64_t keys, int max_tokens, hipStream_t stream) {
   const int64_t blocks = (int64_t)a.tiles * a.Hkv;
@@ -1088,7 +1195,9 @@ hipError_t launch_rows(AttnArgs a, int64_t keys, int max_tokens, hipStream_t str
     grid.x = 512;
   } else {
     const int64_t least = ones ? GROUP : 256;
-    int64_t splits = small ? groups : (256 + blocks - 1) / blocks;
+    int64_t splits = small                  ? groups
+                     : ones || blocks <= 64 ? (256 + blocks - 1) / blocks
+                                            : 512 / blocks;
     splits = std::min({splits, (keys + least - 1) / least, (int64_t)MAX_SPLITS,
                        (int64_t)KV_PART_ROWS / (blocks * a.prow)});
     if (splits < 1 || blocks > KV_MAX_BLOCKS) splits = 1;
@@ -1108,10 +1217,21 @@ hipError_t launch_rows(AttnArgs a, int64_t keys, int max_tokens, hipStream_t str
   return go(attn_rows_kernel<T, DP, false, false>);
 }
 
+// Tiles reach three to four times the rate of row blocks, but a step of theirs
+// takes 1.6 us however few there are, and a tile with few rows is mostly empty.
+// Us in row blocks / in tiles (bf16, D 128, heads over key-value heads):
+//   32 over 8, 512 tokens                  18 / 18    (8.4e6 pairs at most)
+//   32 over 8,  64 tokens behind 2000      23 / 24    (4.2e6)
+//   32 over 8, 256 tokens behind 2000      46 / 36    (18e6)
+//    4 over 4,  64 tokens behind 32000     40 / 63    (8.2e6)
+//   64 over 8,   8 tokens behind 32000     88 / 65    (16e6)
+//   64 over 8, 128 tokens behind 32000    546 / 98    (263e6)
+//   32 over 32, 17 tokens behind 32000    105 / 116, 32 tokens 131 / 116
 template <class T>
 hipError_t launch_attn_t(AttnArgs& a, int64_t keys, int max_tokens, hipStream_t stream) {
   if constexpr (T::V == 8) {
-    if (a.b.cu && (int64_t)max_tokens * a.G > 64) {
+    const int64_t most = (int64_t)a.b.n_tokens * a.G * a.Hkv * keys;  // pairs of query and key
+    if (a.b.cu && max_tokens > 1 && (int64_t)max_tokens * a.G >= 32 && most > 10000000) {
       if (a.D <= 64) return launch_tile<T, 64>(a, stream);
       if (a.D <= 128) return launch_tile<T, 128>(a, stream);
       return launch_tile<T, 256>(a, stream);

@@ -17,13 +17,14 @@ namespace np {
 //                  [S] each: first place and split flag of a row
 //   zeros          KV_ZEROS bytes that stay 0: what stands in for a page that a
 //                  table does not name (eight rows of 256 fp32)
-//   counts         int32 [KV_MAX_BLOCKS]: arrivals of a split row block's
+//   counts         int32 [KV_MAX_BLOCKS]: arrivals of a split block's
 //                  workgroups, 0 between calls
 //   partials       of split attention rows: fp32 [KV_PART_ROWS][DP] outputs,
-//                  then fp32 [KV_PART_ROWS][2] (maximum, sum)
+//                  then fp32 [KV_PART_ROWS][2] (maximum, sum); as many rows as
+//                  two tiles of 128 on every compute unit, split in two
 // ---------------------------------------------------------------------------
 constexpr size_t WS_KV_COPIES = 512;
-constexpr int KV_PART_ROWS = 65536;
+constexpr int KV_PART_ROWS = 131072;
 constexpr size_t KV_ZEROS = 8192;
 constexpr int KV_MAX_BLOCKS = 8192;
 constexpr int KV_MAX_SEQS = 4096;

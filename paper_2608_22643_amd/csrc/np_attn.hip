@@ -1062,12 +1062,14 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
     const uint32_t block = (uint32_t)rank * a.Hkv + h, slot0 = block * a.splits;
     auto at = [&](int c, int i) { return (((slot0 + c) * NO + i) * TILE_T + tid) * 16; };
     uint64_t* const ml = (uint64_t*)a.ml + (size_t)slot0 * TB + wave * 32 + r;
+    const bool live = wave * 32 < t.nrow;  // a wave past the tile's rows has nothing to join
+    if (live)
 #pragma unroll
-    for (int i = 0; i < NO; ++i)
-      buf_store16_agent(prs, at(split, i),
-                        make_float4(o[i / 4][i % 4 * 4], o[i / 4][i % 4 * 4 + 1],
-                                    o[i / 4][i % 4 * 4 + 2], o[i / 4][i % 4 * 4 + 3]));
-    if (h2 == 0)
+      for (int i = 0; i < NO; ++i)
+        buf_store16_agent(prs, at(split, i),
+                          make_float4(o[i / 4][i % 4 * 4], o[i / 4][i % 4 * 4 + 1],
+                                      o[i / 4][i % 4 * 4 + 2], o[i / 4][i % 4 * 4 + 3]));
+    if (live && h2 == 0)
       __hip_atomic_store(ml + split * TB, (uint64_t)__float_as_uint(l) << 32 | __float_as_uint(m),
                          __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -1081,47 +1083,47 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
         __hip_atomic_store(count, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __syncthreads();
-    if (!*s_last) return;
-    auto stats = [&](int c, float* mc, float* lc) {
-      const uint64_t v =
-          __hip_atomic_load(ml + c * TB, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      *mc = __uint_as_float((uint32_t)v);
-      *lc = __uint_as_float((uint32_t)(v >> 32));
+    if (!*s_last || !live) return;
+    // a round trip past the L2 takes about a microsecond: several loads at once
+    auto stats = [&](int c) {
+      return __hip_atomic_load(ml + min(c, parts - 1) * TB, __ATOMIC_RELAXED,
+                               __HIP_MEMORY_SCOPE_AGENT);
     };
-    float M = -INFINITY, L = 0.f, mc, lc;
-    for (int c = 0; c < parts; ++c) {
-      stats(c, &mc, &lc);
-      M = fmaxf(M, mc);
+    float M = -INFINITY;
+    for (int c = 0; c < parts; c += 8) {
+      uint64_t v[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) v[x] = stats(c + x);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) M = fmaxf(M, __uint_as_float((uint32_t)v[x]));
     }
-    f32x16 sum[DT];
+    l = 0.f;
 #pragma unroll
-    for (int j = 0; j < DT; ++j) sum[j] = (f32x16)(0.f);
-    for (int c = 0; c < parts; ++c) {
-      stats(c, &mc, &lc);
-      // without a maximum the sum is 0, or NaN when every score was
-      const float f = mc == -INFINITY ? lc : __builtin_amdgcn_exp2f(mc - M);
-      L += f * lc;
-      float4 v[NO];
-      if (c != split) {
+    for (int j = 0; j < DT; ++j) o[j] = (f32x16)(0.f);
+    for (int c = 0; c < parts; c += 2) {
+      const uint64_t st[2] = {stats(c), stats(c + 1)};
+      float4 v[2][NO];
 #pragma unroll
-        for (int i = 0; i < NO; ++i) v[i] = buf_load16_agent(prs, at(c, i));
-      } else {
+      for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int i = 0; i < NO; ++i)
-          v[i] = make_float4(o[i / 4][i % 4 * 4], o[i / 4][i % 4 * 4 + 1], o[i / 4][i % 4 * 4 + 2],
-                             o[i / 4][i % 4 * 4 + 3]);
-      }
+          v[x][i] = buf_load16_agent(prs, c + x < parts ? at(c + x, i) : BUF_OOB);
 #pragma unroll
-      for (int i = 0; i < NO; ++i) {
-        sum[i / 4][i % 4 * 4] += f * v[i].x;
-        sum[i / 4][i % 4 * 4 + 1] += f * v[i].y;
-        sum[i / 4][i % 4 * 4 + 2] += f * v[i].z;
-        sum[i / 4][i % 4 * 4 + 3] += f * v[i].w;
+      for (int x = 0; x < 2; ++x) {
+        const float mc = __uint_as_float((uint32_t)st[x]);
+        const float lc = c + x < parts ? __uint_as_float((uint32_t)(st[x] >> 32)) : 0.f;
+        // without a maximum the sum is 0, or NaN when every score was
+        const float f = mc == -INFINITY ? lc : __builtin_amdgcn_exp2f(mc - M);
+        l += f * lc;
+#pragma unroll
+        for (int i = 0; i < NO; ++i) {
+          o[i / 4][i % 4 * 4] += f * v[x][i].x;
+          o[i / 4][i % 4 * 4 + 1] += f * v[x][i].y;
+          o[i / 4][i % 4 * 4 + 2] += f * v[x][i].z;
+          o[i / 4][i % 4 * 4 + 3] += f * v[x][i].w;
+        }
       }
     }
-    l = L;
-#pragma unroll
-    for (int j = 0; j < DT; ++j) o[j] = sum[j];
   }
   if (wave * 32 + r >= t.nrow) return;
   const bool none = l == 0.f;  // a row that sees nothing is zero
@@ -1141,10 +1143,11 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
 }
 
 // The keys of a tile are split while the tiles do not give every compute unit two
-// workgroups (64 tokens of 32 heads over 8 behind 32000 others: 774 us unsplit,
-// 96 in 16 parts), but into 32 parts at most and 256 keys at least: the join costs
-// about 1.5 us a part (17 tokens there: 65 in 32 parts, 89 in 64; behind 2000 24
-// with 256 keys a part, 28 with 512).
+// workgroups (64 tokens of 32 heads over 8 behind 32000 others: 774 us unsplit, 75
+// split; 256 tokens behind 2000: 63 and 30), but into 32 parts at most and 256 keys
+// at least: the join costs about 0.6 us a part (8 tokens of 64 heads over 8 behind
+// 32000: 48 in 32 parts, 54 in 64; 256 tokens of 32 over 8 behind 2000: 30 with
+// 256 keys a part, 35 with 512).
 template <class T, int DP>
 hipError_t launch_tile(AttnArgs a, hipStream_t stream) {
   constexpr int KB = TileCfg<DP>::KB;
@@ -1220,15 +1223,17 @@ hipError_t launch_rows(AttnArgs a, int64_t keys, int max_tokens, hipStream_t str
 }
 
 // Tiles reach three to four times the rate of row blocks, but a step of theirs
-// takes 1.6 us however few there are, and a tile with few rows is mostly empty.
-// Us in row blocks / in tiles (bf16, D 128, heads over key-value heads):
-//   32 over 8, 512 tokens                  18 / 18    (8.4e6 pairs at most)
-//   32 over 8,  64 tokens behind 2000      23 / 24    (4.2e6)
-//   32 over 8, 256 tokens behind 2000      46 / 36    (18e6)
-//    4 over 4,  64 tokens behind 32000     40 / 63    (8.2e6)
-//   64 over 8,   8 tokens behind 32000     88 / 65    (16e6)
-//   64 over 8, 128 tokens behind 32000    546 / 98    (263e6)
-//   32 over 32, 17 tokens behind 32000    105 / 116, 32 tokens 131 / 116
+// takes 1.2 to 1.6 us however few there are, and a tile with few rows is mostly
+// empty.  Us in row blocks / in tiles (bf16, D 128, heads over key-value heads; in
+// brackets the most pairs of query and key the host can tell):
+//   32 over 8,  512 tokens                 18.6 / 17.5   (8.4e6)
+//    4 over 4, 1000 tokens                 19.1 / 20.4   (4.0e6)
+//   32 over 8,  128 tokens behind 2000     24.3 / 26.3   (8.7e6)
+//   32 over 8,  256 tokens behind 2000     46.0 / 30.4   (18e6)
+//    4 over 4,   64 tokens behind 32000    35.2 / 45.9   (8.2e6)
+//   64 over 8,    8 tokens behind 32000    90.8 / 48.8   (16e6)
+//   64 over 8,  128 tokens behind 32000     552 / 166    (263e6)
+//   32 over 32,   8 tokens behind 32000    89.9 / 100.5; 17: 107.8 / 100.6
 template <class T>
 hipError_t launch_attn_t(AttnArgs& a, int64_t keys, int max_tokens, hipStream_t stream) {
   if constexpr (T::V == 8) {

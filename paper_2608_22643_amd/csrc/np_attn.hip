@@ -749,10 +749,12 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(
 //
 // 128 rows, so that a step's products (32 cycles a wave and matrix instruction)
 // cover the loads of the next; 64 keys, so that two workgroups fit a compute unit
-// and one's softmax runs beside the other's products.  Bound by the issue of the
-// exponentials and roundings beside the products: 16384 bf16 tokens with 64 heads
-// of 128 4.55 ms, 967 TFLOP/s (an 8192^3 library product reaches 1140); 2048 fp16
-// tokens and 32 heads 65 us (528 TFLOP/s: 1.6 to 2.2 us a step, in line).
+// and one's softmax runs beside the other's products.  No single part bounds it:
+// without the LDS reads of V 16384 bf16 tokens with 64 heads of 128 take 6% less,
+// without exponentials 5%, without loads 12%.  Those take 4.5 to 5.0 ms, 880 to
+// 980 TFLOP/s (an 8192^3 library product reaches 1140 to 1400, from card to card);
+// 2048 fp16 tokens and 32 heads 65 us (528 TFLOP/s; a library product of as many
+// operations 52 to 57 us).
 // Measured and dropped: one workgroup of eight waves in two groups half a step
 // apart, 4.68 to 5.05 ms; the next step's score products dealt between this step's
 // exponentials, 4.56 ms (16384 tokens) and 119 against 106 us (packed prompts).

@@ -110,24 +110,15 @@ struct ExtendArgs {
 __global__ __launch_bounds__(PT) void kv_extend_kernel(ExtendArgs a) {
   extern __shared__ int32_t lds[];
   __shared__ uint32_t scan[PT / WAVE];
+  __shared__ int s_shared;  // some row's last page is
   int32_t* owner = lds;
   int32_t* off = lds + a.S;
   const int tid = threadIdx.x;
+  if (tid == 0) s_shared = 0;
   name_owners(owner, a.S, a.seqs, a.n);
-  // the marks of every shared last page, cleared by whoever will set them
-  // (all writers write the same value)
-  for (int i = tid; i < a.n; i += PT) {
-    const int s = a.seqs ? a.seqs[i] : i;
-    if (s < 0 || s >= a.S || owner[s] != i) continue;
-    const int len = a.st.kv_len[s];
-    if (len <= 0 || len >= a.M * a.P || len % a.P == 0) continue;
-    const int pg = a.st.page_table[(size_t)s * a.M + len / a.P];
-    if (pg < 0 || pg >= a.N) continue;
-    __hip_atomic_store(&a.k.mark[pg], INT_MAX, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __hip_atomic_store(&a.k.cnt[pg], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  __syncthreads();
-  // k.split[i]: -1 left out, else the page its tokens are copied from + 1, or 0
+  // k.split[i]: -1 left out, 0 nothing to copy, else 1 + the last page, partly
+  // filled and held by others too; its marks are cleared by all who will set
+  // them (every writer writes the same value)
   for (int i = tid; i < a.n; i += PT) {
     const int s = a.seqs ? a.seqs[i] : i;
     const int nn = a.n_new ? a.n_new[i] : 1;
@@ -148,16 +139,26 @@ __global__ __launch_bounds__(PT) void kv_extend_kernel(ExtendArgs a) {
         if (pg < 0 || pg >= a.N || a.st.refs[pg] < 1) {
           raise(a.err, NP_DEVERR_STATE);
           split = -1;
-        } else {
-          atomicMin(&a.k.mark[pg], i);
-          atomicAdd(&a.k.cnt[pg], 1);
+        } else if (a.st.refs[pg] > 1) {
+          __hip_atomic_store(&a.k.mark[pg], INT_MAX, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          __hip_atomic_store(&a.k.cnt[pg], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
           split = pg + 1;
+          s_shared = 1;
         }
       }
     }
     a.k.split[i] = split;
   }
   __syncthreads();
+  if (s_shared) {
+    for (int i = tid; i < a.n; i += PT) {
+      const int split = a.k.split[i];
+      if (split <= 0) continue;
+      atomicMin(&a.k.mark[split - 1], i);
+      atomicAdd(&a.k.cnt[split - 1], 1);
+    }
+    __syncthreads();
+  }
   // how many pages each row needs, and where its pages start in the list
   int total = 0, copies = 0;
   for (int base = 0; base < a.n; base += PT) {
@@ -169,9 +170,9 @@ __global__ __launch_bounds__(PT) void kv_extend_kernel(ExtendArgs a) {
       // past N the call is refused whatever the rest needs: sums stay in range
       need = min(div_up(len + nn, a.P) - div_up(len, a.P), a.N + 1);
       if (split > 0) {
-        const int pg = split - 1, refs = a.st.refs[pg];
-        const bool keeps = refs == 1 || (refs == fresh(&a.k.cnt[pg]) && fresh(&a.k.mark[pg]) == i);
-        if (keeps) split = 0;
+        // when all its holders are rows of this call, the first keeps it
+        const int pg = split - 1;
+        if (a.st.refs[pg] == fresh(&a.k.cnt[pg]) && fresh(&a.k.mark[pg]) == i) split = 0;
         else ++need;
         a.k.split[i] = split;
       }

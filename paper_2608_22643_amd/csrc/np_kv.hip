@@ -7,8 +7,8 @@
 // counts -> free pages), so latency bounds them and the host never has to
 // wait for a count.  A split over workgroups would add a trip past the L2
 // (microseconds) between any two of those steps.  Measured: 16 sequences of
-// up to 2001 tokens in pages of 64: extend 7.8 us, fork 3.0, free 2.4; the
-// plan of a compaction of 48 sequences 5.4.  The page bytes they decide about
+// up to 2001 tokens in pages of 64: extend 7.4 us, fork 2.8, free 2.4; the
+// plan of a compaction of 48 sequences 5.6.  The page bytes they decide about
 // are moved by a second kernel over the whole card, which reads how many pages
 // there are from the device, as np_stage_gather does with its lists.
 #include <limits.h>

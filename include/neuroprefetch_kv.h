@@ -132,9 +132,11 @@ typedef struct np_rotary {
 np_status np_kv_shape_check(const np_kv_shape* shape);
 
 /* Bytes of device workspace ("dev_ws") the calls below need: one workspace
- * per stream of calls, zeroed or given to np_kv_reset before its first use.
- * It starts with the sticky error word that np_device_error reads.  Host
- * only. */
+ * per stream of calls, zeroed or given to np_kv_reset (of any shape) before
+ * its first use.  It starts with the sticky error word that np_device_error
+ * reads.  Caches of several shapes may take turns on one workspace of at least
+ * the largest size any of them needs; the error word is then theirs together.
+ * The calls of neuroprefetch.h need a workspace of their own.  Host only. */
 np_status np_kv_workspace_size(const np_kv_shape* shape, size_t* dev_ws_bytes);
 
 /* An empty cache: page_table -1, kv_len 0, refs 0, error word cleared.  The

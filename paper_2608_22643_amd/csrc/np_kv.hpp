@@ -12,16 +12,19 @@ namespace np {
 // Workspace of the cache and attention calls.
 //   [0, 4096)      control block: the error word (as in every workspace) and
 //                  +512 the number of entries of the copy list
-//   page scratch   int32 [N] each: free pages, copy sources, copy targets,
-//                  copied tokens, page renaming, two marks per page; int32
-//                  [S] each: first place and split flag of a row
 //   zeros          KV_ZEROS bytes that stay 0: what stands in for a page that a
 //                  table does not name (eight rows of 256 fp32)
 //   counts         int32 [KV_MAX_BLOCKS]: arrivals of a split block's
 //                  workgroups, 0 between calls
+//   page scratch   int32 [N] each: free pages, copy sources, copy targets,
+//                  copied tokens, page renaming, two marks per page; int32
+//                  [S] each: first place and split flag of a row
 //   partials       of split attention rows: fp32 [KV_PART_ROWS][DP] outputs,
 //                  then fp32 [KV_PART_ROWS][2] (maximum, sum); as many rows as
 //                  two tiles of 128 on every compute unit, split in two
+// Zeros and counts have to last from call to call, so they come before
+// everything whose size depends on the shape: one workspace serves caches of
+// several shapes in turn.
 // ---------------------------------------------------------------------------
 constexpr size_t WS_KV_COPIES = 512;
 constexpr int KV_PART_ROWS = 131072;
@@ -45,11 +48,11 @@ inline size_t kv_ws_layout(const np_kv_shape& s, char* ws, KvScratch* k) {
     return p;
   };
   KvScratch t;
+  t.zeros = take(KV_ZEROS);
+  t.count = (int32_t*)take(KV_MAX_BLOCKS * 4);
   for (int32_t** p : {&t.free_ids, &t.src, &t.dst, &t.rows, &t.remap, &t.mark, &t.cnt})
     *p = (int32_t*)take((size_t)s.n_pages * 4);
   for (int32_t** p : {&t.off, &t.split}) *p = (int32_t*)take((size_t)(s.max_seqs + 1) * 4);
-  t.zeros = take(KV_ZEROS);
-  t.count = (int32_t*)take(KV_MAX_BLOCKS * 4);
   t.part = (float*)take((size_t)KV_PART_ROWS * kv_dpad(s.head_dim) * 4);
   t.ml = (float*)take((size_t)KV_PART_ROWS * 2 * 4);
   if (k) *k = t;

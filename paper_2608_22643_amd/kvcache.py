@@ -2,8 +2,8 @@
 runtime around the cache and attention kernels).
 
 KVCache owns the device buffers of a cache (torch allocations) and forwards to
-the np_kv_* and np_attn_* calls on one stream; sequences are rows of its page
-table.  A step is
+the np_kv_* and np_attn_* calls on one stream, in order with the stream its
+caller is on; sequences are rows of its page table.  A step is
 
     extend (pages for the new tokens) -> per layer: append -> attention
 
@@ -18,6 +18,7 @@ samples that share its pages, decodes them, frees them and compacts the pool:
 """
 from __future__ import annotations
 
+import contextlib
 import math
 
 import numpy as np
@@ -39,8 +40,16 @@ def rotary_tables(dim: int, max_pos: int, theta: float = 10000.0, device="cuda:0
 class KVCache:
     """Pages, page table, lengths and reference counts of up to max_seqs
     sequences of at most max_len tokens, n_pages pages of page_size tokens in
-    every layer.  All calls are enqueued on `stream` (default: the null
-    stream); lists of sequences may be Python lists or device int32 tensors."""
+    every layer.
+
+    All calls are enqueued on `stream` (a torch stream or a handle; default: the
+    device's default stream), which every buffer of the cache and of its
+    batches belongs to.  Called while another stream is current, a call starts
+    after what that one holds, and it goes on after the call: inputs and
+    outputs need no events, and may be dropped as soon as the call returns.
+
+    Sequences, prefix lengths: Python lists (uploaded from pageable memory, which
+    waits for the stream) or contiguous int32 tensors on the device."""
 
     def __init__(self, layers: int, heads: int, kv_heads: int, head_dim: int, dtype: str, max_seqs: int, max_len: int,
                  page_size: int = 64, n_pages: int | None = None, device: str = "cuda:0", stream=None,
@@ -49,68 +58,108 @@ class KVCache:
         n_pages = max_seqs * seq_pages if n_pages is None else n_pages
         self.shape = B.make_kv_shape(layers, heads, kv_heads, head_dim, page_size, n_pages, max_seqs, seq_pages, dtype)
         B.np_kv_shape_check(self.shape)
-        self.device, self.stream = torch.device(device), stream
+        self.device = torch.device(device)
+        if stream is None or stream == 0:
+            stream = torch.cuda.default_stream(self.device)
+        elif isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, self.device)
+        self.stream = stream
         self.max_len = seq_pages * page_size
-        i32 = dict(dtype=torch.int32, device=self.device)
-        self.page_table = torch.empty(max_seqs, seq_pages, **i32)
-        self.kv_len, self.refs = torch.empty(max_seqs, **i32), torch.empty(n_pages, **i32)
-        self.state = B.make_kv_state(self.page_table, self.kv_len, self.refs)
-        self.pool = torch.empty(layers, n_pages, 2, kv_heads, page_size, head_dim, dtype=TORCH_DT[dtype],
-                                device=self.device)
-        self.ws = torch.zeros(B.np_kv_workspace_size(self.shape), dtype=torch.uint8, device=self.device)
         self.scale = 1.0 / math.sqrt(head_dim)
         self.rotary = None
-        if rotary_dim:
-            self.rotary = B.make_rotary(*rotary_tables(rotary_dim, self.max_len, device=self.device))
-        self.reset()
+        with self.on_stream():
+            i32 = dict(dtype=torch.int32, device=self.device)
+            self.page_table = torch.empty(max_seqs, seq_pages, **i32)
+            self.kv_len, self.refs = torch.empty(max_seqs, **i32), torch.empty(n_pages, **i32)
+            self.state = B.make_kv_state(self.page_table, self.kv_len, self.refs)
+            self.pool = torch.empty(layers, n_pages, 2, kv_heads, page_size, head_dim, dtype=TORCH_DT[dtype],
+                                    device=self.device)
+            self.ws = torch.zeros(B.np_kv_workspace_size(self.shape), dtype=torch.uint8, device=self.device)
+            if rotary_dim:
+                self.rotary = B.make_rotary(*rotary_tables(rotary_dim, self.max_len, device=self.device))
+            self.reset()
+
+    @contextlib.contextmanager
+    def on_stream(self):
+        """Makes the cache's stream the current one, after what the caller's
+        stream holds; on leaving, the caller's stream goes on after it.  So a
+        block that either stream's allocator hands out again is written after
+        the other's last use of it."""
+        here = torch.cuda.current_stream(self.device)
+        if here.cuda_stream == self.stream.cuda_stream:
+            yield
+            return
+        self.stream.wait_stream(here)
+        try:
+            with torch.cuda.stream(self.stream):
+                yield
+        finally:
+            here.wait_stream(self.stream)
 
     def _ids(self, x):
-        if x is None or isinstance(x, torch.Tensor):
+        if x is None:
+            return None
+        if isinstance(x, torch.Tensor):
+            if x.dtype != torch.int32 or not x.is_cuda or not x.is_contiguous():
+                raise ValueError("need a list or a contiguous int32 tensor on the device")
+            x.record_stream(self.stream)  # a batch may be read after calls from other streams
             return x
         return torch.tensor(list(x), dtype=torch.int32, device=self.device)
 
     def reset(self) -> None:
-        B.np_kv_reset(self.shape, self.state, self.ws, self.stream)
+        with self.on_stream():
+            B.np_kv_reset(self.shape, self.state, self.ws, self.stream)
 
     def extend(self, seqs, n_new: list[int] | None = None, max_len: int | None = None) -> B.np_kv_batch:
-        """Pages for n_new[b] tokens of sequence seqs[b] (default: one each);
-        returns the step's batch for append, prompt and decode.  max_len: a
-        bound on the lengths after the step, if the caller knows one."""
-        seqs = list(seqs)
-        n = len(seqs)
-        dev_seqs = self._ids(seqs)
-        pos0 = torch.empty(n, dtype=torch.int32, device=self.device)
-        new = self._ids(n_new)
-        B.np_kv_extend(self.shape, self.state, self.pool, n, dev_seqs, new, pos0, self.ws, self.stream)
-        most = self.max_len if max_len is None else max_len
-        if n_new is None:
-            return B.make_kv_batch(n, n, 1, most, pos0, seqs=dev_seqs)
-        cu = self._ids(np.concatenate([[0], np.cumsum(n_new)]).tolist())
-        return B.make_kv_batch(n, sum(n_new), max(n_new), most, pos0, seqs=dev_seqs, cu_tokens=cu)
+        """Pages for n_new[b] tokens of sequence seqs[b] (default: one each; a
+        list, since the host needs their sum); returns the step's batch for
+        append, prompt and decode.  max_len: a bound on the lengths after the
+        step, if the caller knows one."""
+        with self.on_stream():
+            seqs = self._ids(seqs)
+            n = seqs.numel()
+            if n_new is not None and len(n_new) != n:
+                raise ValueError(f"{len(n_new)} token counts for {n} sequences")
+            pos0 = torch.empty(n, dtype=torch.int32, device=self.device)
+            B.np_kv_extend(self.shape, self.state, self.pool, n, seqs, self._ids(n_new), pos0, self.ws, self.stream)
+            most = self.max_len if max_len is None else max_len
+            if n_new is None:
+                return B.make_kv_batch(n, n, 1, most, pos0, seqs=seqs)
+            cu = self._ids(np.concatenate([[0], np.cumsum(n_new)]).tolist())
+            return B.make_kv_batch(n, sum(n_new), max(n_new), most, pos0, seqs=seqs, cu_tokens=cu)
 
     def fork(self, src, dst, lens=None) -> None:
-        src = self._ids(src)
-        B.np_kv_fork(self.shape, self.state, src.numel(), src, self._ids(dst), self._ids(lens), self.ws, self.stream)
+        with self.on_stream():
+            src, dst, lens = self._ids(src), self._ids(dst), self._ids(lens)
+            if dst.numel() != src.numel() or (lens is not None and lens.numel() != src.numel()):
+                raise ValueError("src, dst and lens differ in length")
+            B.np_kv_fork(self.shape, self.state, src.numel(), src, dst, lens, self.ws, self.stream)
 
     def free(self, seqs) -> None:
-        seqs = self._ids(seqs)
-        B.np_kv_free(self.shape, self.state, seqs.numel(), seqs, self.ws, self.stream)
+        with self.on_stream():
+            seqs = self._ids(seqs)
+            B.np_kv_free(self.shape, self.state, seqs.numel(), seqs, self.ws, self.stream)
 
     def compact(self) -> None:
-        B.np_kv_compact(self.shape, self.state, self.pool, None, self.ws, self.stream)
+        with self.on_stream():
+            B.np_kv_compact(self.shape, self.state, self.pool, None, self.ws, self.stream)
 
     def append(self, layer: int, batch, q, k, v, q_out) -> None:
-        B.np_kv_append(self.shape, layer, batch, self.page_table, B.make_qkv(q, k, v, q_out), self.rotary, self.pool,
-                       self.ws, self.stream)
+        with self.on_stream():
+            B.np_kv_append(self.shape, layer, batch, self.page_table, B.make_qkv(q, k, v, q_out), self.rotary,
+                           self.pool, self.ws, self.stream)
 
     def attend(self, layer: int, batch, q, out, window: int = 0) -> None:
         """Attention of the batch's tokens; the keys and values of its new
         tokens have been appended."""
         call = B.np_attn_prompt if batch.cu_tokens else B.np_attn_decode
-        call(self.shape, layer, batch, self.page_table, q, self.pool, self.scale, window, out, self.ws, self.stream)
+        with self.on_stream():
+            call(self.shape, layer, batch, self.page_table, q, self.pool, self.scale, window, out, self.ws,
+                 self.stream)
 
     def pages_used(self) -> int:
-        return int((self.refs > 0).sum())
+        with self.on_stream():
+            return int((self.refs > 0).sum())
 
     def device_error(self) -> int:
         return B.np_device_error(self.ws, self.stream)
@@ -119,31 +168,33 @@ class KVCache:
 class DecoderLayers:
     """cfg.layers whole decoder layers with synthetic weights: x += Wo attention(
     norm(x)), x += MLP(norm(x)), norm(x) = x / rms(x); the MLP from the
-    configuration's neuron records.  Everything runs on the null stream."""
+    configuration's neuron records.  Everything runs on the cache's stream, in
+    order with the caller's as KVCache's calls are."""
 
     def __init__(self, cfg: W.Config, heads: int, kv_heads: int, max_seqs: int, max_len: int, page_size: int = 64,
-                 window: int = 0, device: str = "cuda:0", n_pages: int | None = None):
+                 window: int = 0, device: str = "cuda:0", n_pages: int | None = None, stream=None):
         d, dt = cfg.d_model, TORCH_DT[cfg.adtype]
         self.cfg, self.heads, self.kv_heads, self.head_dim, self.window = cfg, heads, kv_heads, d // heads, window
         self.device = torch.device(device)
         self.cache = KVCache(cfg.layers, heads, kv_heads, self.head_dim, cfg.adtype, max_seqs, max_len, page_size,
-                             n_pages, device, rotary_dim=self.head_dim // 16 * 16)
+                             n_pages, device, stream, rotary_dim=self.head_dim // 16 * 16)
         g = torch.Generator().manual_seed(cfg.seed + 17)
         width = (heads + 2 * kv_heads) * self.head_dim
 
         def normal(rows, cols):
             return (torch.randn(rows, cols, generator=g) / math.sqrt(rows)).to(dt).to(self.device)
 
-        self.wqkv = [normal(d, width) for _ in range(cfg.layers)]
-        self.wo = [normal(d, d) for _ in range(cfg.layers)]
-        self.records = []  # per layer [F][3d], resident
-        for layer in range(cfg.layers):
-            r = W.storage(cfg, layer, 1)[0]
-            t = torch.from_numpy(r.view(np.int16) if cfg.wdtype != "f32" else r).to(self.device)
-            self.records.append(t.view(dt) if cfg.wdtype != "f32" else t)
-        self.mlp_shape = B.make_shape(cfg.layers, d, cfg.d_ffn, cfg.rank, cfg.k, cfg.capacity, cfg.wdtype, cfg.adtype,
-                                      cfg.act)
-        self.mlp_ws = torch.zeros(B.np_workspace_size(self.mlp_shape), dtype=torch.uint8, device=self.device)
+        with self.cache.on_stream():
+            self.wqkv = [normal(d, width) for _ in range(cfg.layers)]
+            self.wo = [normal(d, d) for _ in range(cfg.layers)]
+            self.records = []  # per layer [F][3d], resident
+            for layer in range(cfg.layers):
+                r = W.storage(cfg, layer, 1)[0]
+                t = torch.from_numpy(r.view(np.int16) if cfg.wdtype != "f32" else r).to(self.device)
+                self.records.append(t.view(dt) if cfg.wdtype != "f32" else t)
+            self.mlp_shape = B.make_shape(cfg.layers, d, cfg.d_ffn, cfg.rank, cfg.k, cfg.capacity, cfg.wdtype,
+                                          cfg.adtype, cfg.act)
+            self.mlp_ws = torch.zeros(B.np_workspace_size(self.mlp_shape), dtype=torch.uint8, device=self.device)
 
     def _norm(self, x):
         f = x.float()
@@ -153,15 +204,23 @@ class DecoderLayers:
         rec, d, n = self.records[layer], self.cfg.d_model, x.shape[0]
         if n > 16:  # a prompt: the activations on the matrix cores, then the down rows
             acts = torch.empty(n, self.cfg.d_ffn, dtype=torch.float32, device=self.device)
-            B.np_act_batch(self.mlp_shape, rec, x, n, acts)
+            B.np_act_batch(self.mlp_shape, rec, x, n, acts, None, self.cache.stream)
             return (acts @ rec[:, 2 * d:].float()).to(x.dtype)
         y = torch.empty_like(x)
         for i in range(n):
-            B.np_dense_mlp(self.mlp_shape, rec, x[i], y[i], self.mlp_ws)
+            B.np_dense_mlp(self.mlp_shape, rec, x[i], y[i], self.mlp_ws, self.cache.stream)
         return y
 
     def step(self, x, batch):
         """The layers over x [tokens][d_model] for a batch of KVCache.extend."""
+        here = torch.cuda.current_stream(self.device)
+        with self.cache.on_stream():
+            x = self._layers(x, batch)
+        if here.cuda_stream != self.cache.stream.cuda_stream:
+            x.record_stream(here)
+        return x
+
+    def _layers(self, x, batch):
         hq, hk, hd = self.heads, self.kv_heads, self.head_dim
         for layer in range(self.cfg.layers):
             qkv = (self._norm(x) @ self.wqkv[layer]).view(-1, hq + 2 * hk, hd)

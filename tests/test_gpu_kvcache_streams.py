@@ -1,0 +1,154 @@
+"""KVCache and DecoderLayers called from other streams than their own: lists
+and inputs are dropped as soon as a call returns, their memory is written again
+at once, and nothing waits for the device in between."""
+import random
+
+import pytest
+import torch
+
+from kv_ref import PageModel, attention
+from paper_2608_22643_amd import binding as B
+from paper_2608_22643_amd import kvcache
+from paper_2608_22643_amd import workload as W
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BUSY = 200_000  # clock cycles that hold a stream up, so that what follows in it waits
+
+
+def streams(kind):
+    """(the stream the cache is given, the stream its caller is on)"""
+    side = torch.cuda.Stream()
+    return {"cache beside": (side, torch.cuda.default_stream()),
+            "caller beside": (None, side),
+            "a handle": (side.cuda_stream, torch.cuda.default_stream()),
+            "two beside": (torch.cuda.Stream(), side),
+            "one": (side, side)}[kind]
+
+
+def scribble(sizes=(1, 2, 3, 5, 9, 40)):
+    """Takes what the caller's stream has free and fills it with what no list
+    may hold."""
+    for n in sizes:
+        for _ in range(4):
+            torch.full((n,), 1 << 30, dtype=torch.int32, device=DEV)
+
+
+@pytest.mark.parametrize("kind", ["cache beside", "caller beside", "a handle", "two beside", "one"])
+def test_lists_live_until_they_are_read(kind):
+    given, here = streams(kind)
+    S, N, P = 9, 60, 16
+    rng = random.Random(7)
+    with torch.cuda.stream(here):
+        c = kvcache.KVCache(2, 1, 1, 8, "f32", S, 12 * P, P, N, stream=given)
+        m = PageModel(S, N, 12, P)
+        got = []
+        for step in range(60):
+            with torch.cuda.stream(c.stream):
+                torch.cuda._sleep(BUSY)
+            op = rng.random()
+            tensors = rng.random() < 0.5
+            put = (lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)) if tensors else list
+            if op < 0.55:
+                seqs = rng.sample(range(S), rng.randint(1, S))
+                new = None if rng.random() < 0.4 else [rng.choice([0, 1, P, rng.randint(1, 2 * P)]) for _ in seqs]
+                batch = c.extend(put(seqs), new)
+                got.append((batch._kept[0], m.extend(seqs, new or [1] * len(seqs))))
+                del batch
+            elif op < 0.75:
+                src, dst = [rng.randrange(S) for _ in range(3)], rng.sample(range(S), 3)
+                lens = None if rng.random() < 0.5 else [rng.randint(0, m.len[s]) for s in src]
+                c.fork(put(src), put(dst), None if lens is None else put(lens))
+                m.fork(src, dst, lens)
+            elif op < 0.92:
+                seqs = rng.sample(range(S), 2)
+                c.free(put(seqs))
+                m.free(seqs)
+            else:
+                c.compact()
+                m.compact()
+            scribble()
+            if step % 20 == 19:
+                assert c.pages_used() == sum(r > 0 for r in m.refs)
+        c.device_error()  # waits for the cache's stream
+        assert c.kv_len.tolist() == m.len and c.refs.tolist() == m.refs
+        assert c.page_table.tolist() == m.tables()
+        for pos0, want in got:
+            assert pos0.tolist() == want
+
+
+@pytest.mark.parametrize("kind", ["cache beside", "caller beside", "two beside"])
+def test_inputs_and_outputs_need_no_events(kind):
+    """Queries, keys and values made on the caller's stream and dropped after
+    the call, outputs read there."""
+    given, here = streams(kind)
+    rows = [(0, 70), (0, 5)]
+    g = torch.Generator().manual_seed(2)
+    host = torch.randn(75, 8, 64, generator=g)
+    with torch.cuda.stream(here):
+        c = kvcache.KVCache(1, 4, 2, 64, "f32", 2, 160, 16, stream=given)
+        for turn in range(4):
+            src = host.to(DEV)
+            batch = c.extend([0, 1], [70, 5])
+            torch.cuda._sleep(BUSY)
+            qkv = src * 1.0  # written late on the caller's stream
+            q = torch.empty(75, 4, 64, device=DEV)
+            with torch.cuda.stream(c.stream):
+                torch.cuda._sleep(BUSY)
+            c.append(0, batch, qkv[:, :4], qkv[:, 4:6], qkv[:, 6:], q)
+            del qkv
+            torch.full((75, 8, 64), float("nan"), device=DEV)
+            out = torch.empty(75, 4, 64, device=DEV)
+            c.attend(0, batch, q, out)
+            del q, batch
+            torch.full((75, 4, 64), float("nan"), device=DEV)
+            scribble()
+            res = out.cpu()
+            at = 0
+            for _, n in rows:
+                x = host[at:at + n]
+                ref, tol = attention(x[:, :4], x[:, 4:6].transpose(0, 1), x[:, 6:].transpose(0, 1), 0, c.scale, 0, "f32")
+                assert ((res[at:at + n].double() - ref).abs() <= tol).all()
+                at += n
+            c.free([0, 1])
+        assert c.device_error() == 0
+
+
+def test_layers_beside_the_caller_give_the_same_bits():
+    cfg = W.get("tiny").with_(layers=2)
+    x = torch.randn(40, cfg.d_model, generator=torch.Generator().manual_seed(3))
+
+    def run(given, here):
+        with torch.cuda.stream(here):
+            net = kvcache.DecoderLayers(cfg, 4, 2, 3, 64, 16, stream=given)
+            dt = kvcache.TORCH_DT[cfg.adtype]
+            outs = []
+            for n in (30, 1, 1):
+                seqs = [0, 2]
+                batch = net.cache.extend(seqs, None if n == 1 else [n, n])
+                h = x[:n].repeat(2, 1).to(dt).to(DEV)
+                torch.cuda._sleep(BUSY)
+                y = net.step(h * 1.0, batch)
+                outs.append((y + 0.0).cpu())
+                del y, batch
+                scribble()
+            assert net.cache.device_error() == 0
+            return torch.cat(outs)
+
+    torch.cuda.synchronize()
+    want = run(None, torch.cuda.default_stream())
+    for kind in ("cache beside", "caller beside", "two beside"):
+        assert torch.equal(run(*streams(kind)), want), kind
+
+
+def test_lists_are_checked():
+    c = kvcache.KVCache(1, 1, 1, 8, "f32", 4, 64, 16)
+    for bad in (torch.tensor([0, 1], device=DEV), torch.tensor([0, 1], dtype=torch.int32),
+                torch.zeros(4, dtype=torch.int32, device=DEV)[::2]):
+        for call in (lambda: c.extend(bad), lambda: c.fork(bad, [2, 3]), lambda: c.free(bad)):
+            with pytest.raises(ValueError):
+                call()
+    for call in (lambda: c.extend([0, 1], [3]), lambda: c.fork([0, 1], [2]), lambda: c.fork([0], [1], [1, 1])):
+        with pytest.raises(ValueError):
+            call()
+    assert c.pages_used() == 0 and c.device_error() == 0

@@ -203,7 +203,9 @@ np_status np_kv_append(const np_kv_shape* shape, int32_t layer, const np_kv_batc
  * with the same stride.  scale: finite.  window >= 0.  Sums, softmax
  * statistics and accumulators are fp32; for 16-bit types the probabilities
  * are rounded to w before they meet the values, as the matrix cores take
- * them.  Memory at positions outside the keys a row's tokens see together may
+ * them.  A NaN or +infinity among a token's scores makes its outputs of that
+ * head NaN; one whose scores are all -infinity gets zeros, as if it saw
+ * nothing.  Memory at positions outside the keys a row's tokens see together may
  * hold anything, NaN and infinities included; a value that is not finite at a
  * position that some token of the row sees may also reach those of its tokens
  * that do not see it (there it is multiplied by a weight of zero).

@@ -905,8 +905,8 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
     if (next_bad)
 #pragma unroll
       for (int i = 0; i < NL; ++i)
-        if (page[i] < 0 || page[i] >= a.N) {  // masked below: any finite row will do
-          p[i] = pv[i] = a.q + (int64_t)t.row.begin * a.q_stride;
+        if (page[i] < 0 || page[i] >= a.N) {  // masked below, but has to be finite
+          p[i] = pv[i] = a.zeros;
           o[i] = lc * 16;
         }
     if (lon) {

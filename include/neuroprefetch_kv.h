@@ -85,9 +85,10 @@ typedef struct np_kv_state {
  * without the host knowing.  Device-side checks: a sequence outside [0, S), a
  * cu_tokens that descends or leaves [0, n_tokens], and a position at or past
  * max_len or M P set NP_DEVERR_STATE, and the row is not served (one whose
- * cu_tokens are bad has no tokens); a page outside [0, N) where a token sees
- * keys sets NP_DEVERR_NOT_RESIDENT (its keys count as not visible).  At most
- * 2^24 tokens and 2^30 query heads in all. */
+ * cu_tokens are bad has no tokens; a token that several others then claim is
+ * appended for the first of them, and its outputs are those of any); a page
+ * outside [0, N) where a token sees keys sets NP_DEVERR_NOT_RESIDENT (its keys
+ * count as not visible).  At most 2^24 tokens and 2^30 query heads in all. */
 typedef struct np_kv_batch {
   int32_t n_seq;
   int32_t n_tokens;

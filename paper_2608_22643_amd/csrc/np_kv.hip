@@ -443,16 +443,24 @@ __global__ __launch_bounds__(APP_T) void kv_append_kernel(AppendArgs a) {
   constexpr int V = T::V;
   constexpr int W = 16 / V;
   const int t = blockIdx.x;
-  // the token's row: how many rows end at or before it
+  // the token's row, as the attention calls have it: the one whose tokens
+  // include it, bad rows (reported with token 0) having none
   int row = t;
   if (a.b.cu) {
-    row = 0;
+    row = -1;
     const int lane = threadIdx.x % WAVE;
-    for (int base = 0; base < a.b.n_seq; base += WAVE) {
-      const bool past = base + lane < a.b.n_seq && a.b.cu[base + lane + 1] <= t;
-      row += __popcll(__ballot(past));
+    for (int base = 0; base < a.b.n_seq && (row < 0 || t == 0); base += WAVE) {
+      bool mine = false;
+      if (base + lane < a.b.n_seq) {
+        const int lo = a.b.cu[base + lane], hi = a.b.cu[base + lane + 1];
+        const bool bad = lo < 0 || hi < lo || hi > a.b.n_tokens;
+        if (bad && t == 0 && threadIdx.x < WAVE) raise(a.err, NP_DEVERR_STATE);
+        mine = !bad && lo <= t && t < hi;
+      }
+      const uint64_t hit = __ballot(mine);
+      if (hit && row < 0) row = base + __ffsll((unsigned long long)hit) - 1;
     }
-    if (row >= a.b.n_seq) return;  // past the last row's tokens
+    if (row < 0) return;  // nobody's token
   }
   row = __builtin_amdgcn_readfirstlane(row);
   int32_t* err = threadIdx.x == 0 ? a.err : nullptr;

@@ -119,7 +119,8 @@ __device__ inline bool find_block_longest(const KvBatch& b, int G, int rank, int
       if (err && rank == 0 && threadIdx.x < WAVE) atomicOr(err, NP_DEVERR_STATE);
     } else {
       n = (int)(((int64_t)(w.hi - w.lo) * G + RB - 1) / RB);
-      lo = (int)((int64_t)min(max(w.p0, 0), b.lim) * G / RB);
+      // rows past level 2^30 (2^37 query heads from their start) share that level
+      lo = (int)min((int64_t)min(max(w.p0, 0), b.lim) * G / RB, (int64_t)1 << 30);
     }
   }
   auto above = [&](int x) {  // blocks of level x or more

@@ -634,7 +634,7 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(
   };
 
   if constexpr (!EVEN) {
-    const int id = blockIdx.x;
+    const int id = grid_block();  // past the last block: a split there is none of
     const int h = id % a.Hkv, tile = id / a.Hkv % a.tiles, split = id / a.Hkv / a.tiles;
     int32_t* const err = split == 0 && h == 0 ? a.err : nullptr;
     int row, blk;
@@ -1211,7 +1211,7 @@ hipError_t launch_rows(AttnArgs a, int64_t keys, int max_tokens, hipStream_t str
     if (splits < 1 || blocks > KV_MAX_BLOCKS) splits = 1;
     a.chunk = (int)(((keys + splits - 1) / splits + GROUP - 1) / GROUP * GROUP);
     a.splits = (int)((keys + a.chunk - 1) / a.chunk);
-    grid.x = (unsigned)(blocks * a.splits);
+    grid = block_grid(blocks * a.splits);
   }
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(ROWS_T), 0, stream, a);

@@ -442,7 +442,8 @@ template <class T, bool INTER>
 __global__ __launch_bounds__(APP_T) void kv_append_kernel(AppendArgs a) {
   constexpr int V = T::V;
   constexpr int W = 16 / V;
-  const int t = blockIdx.x;
+  const int t = grid_block();
+  if (t >= a.b.n_tokens) return;
   // the token's row, as the attention calls have it: the one whose tokens
   // include it, bad rows (reported with token 0) having none
   int row = t;
@@ -671,7 +672,7 @@ hipError_t launch_kv_append(const np_kv_shape& s, int layer, const np_kv_batch& 
   a.err = (int32_t*)((char*)ws + WS_ERR);
   const bool inter = rot && rot->interleaved;
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)b.n_tokens), dim3(APP_T), 0, stream, a);
+    hipLaunchKernelGGL(kernel, block_grid(b.n_tokens), dim3(APP_T), 0, stream, a);
   };
   if (s.dtype == NP_F32) {
     if (inter) go(kv_append_kernel<TF32, true>);

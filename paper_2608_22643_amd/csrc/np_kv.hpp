@@ -130,6 +130,15 @@ __device__ inline KvRow kv_row(const KvBatch& a, int b, int32_t* err) {
   return kv_row_check(a, kv_row_load(a, b), err);
 }
 
+// A grid of at least `blocks` workgroups of up to 256 threads, numbered by
+// grid_block().  A launch may have fewer than 2^32 threads along an axis; the
+// calls allow 2^24 tokens and 2^26 row blocks.
+inline dim3 block_grid(int64_t blocks) {
+  const int64_t x = blocks < (1 << 23) ? blocks : 1 << 23;
+  return dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
+}
+__device__ inline int grid_block() { return (int)(blockIdx.y * gridDim.x + blockIdx.x); }
+
 // ---------------------------------------------------------------------------
 // launchers
 // ---------------------------------------------------------------------------

@@ -1,5 +1,5 @@
 """The ends of the ranges the interface names: positions up to 2^30, groups of
-1024 heads."""
+1024 heads, 2^24 tokens, more than 2^28 query heads in row blocks."""
 import pytest
 import torch
 
@@ -86,3 +86,46 @@ def test_decode_at_far_positions(dtype, rows, window):
 def test_small_prompts_at_far_positions():
     s = Far([(LAST - 9, 9), (1 << 29, 3), (0, 5)], 70, 8, 2, 64, "f32")
     s.check(s.run(B.np_attn_prompt), (0, 7))
+
+
+def test_append_of_the_most_tokens():
+    """2^24 tokens of one sequence, every slot."""
+    T, P = 1 << 24, 256
+    pages = T // P
+    shape = B.make_kv_shape(1, 1, 1, 8, P, pages, 1, pages, "f16")
+    ws = torch.zeros(B.np_kv_workspace_size(shape), dtype=torch.uint8, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    qkv = torch.randint(-30000, 30000, (T, 3, 8), dtype=torch.int16, device=DEV, generator=g).view(torch.float16)
+    pool = torch.zeros(1, pages, 2, 1, P, 8, dtype=torch.float16, device=DEV)
+    out = torch.zeros(T, 1, 8, dtype=torch.float16, device=DEV)
+    batch = B.make_kv_batch(1, T, T, T, i32([0]), cu_tokens=i32([0, T]))
+    B.np_kv_append(shape, 0, batch, i32(range(pages)), B.make_qkv(qkv[:, :1], qkv[:, 1:2], qkv[:, 2:], out), None, pool,
+                   ws)
+    assert B.np_device_error(ws) == 0
+    bits = lambda x: x.reshape(T, 8).view(torch.int16)
+    assert torch.equal(bits(out), bits(qkv[:, 0]))
+    for kind in (0, 1):
+        assert torch.equal(bits(pool[0, :, kind, 0]), bits(qkv[:, 1 + kind]))
+
+
+def test_row_blocks_of_more_than_2_28_query_heads():
+    """A window of one key: every head of a token gives the token's own value
+    vector, exactly."""
+    n, S, Hq, P = 4100, 64, 1024, 256
+    T, M = n * S, 17
+    assert T * Hq // 16 * 256 > 1 << 32  # threads of the launch
+    shape = B.make_kv_shape(1, Hq, 1, 8, P, S * M, S, M, "f32")
+    ws = torch.zeros(B.np_kv_workspace_size(shape), dtype=torch.uint8, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(2)
+    pool = torch.randn(1, S * M, 2, 1, P, 8, device=DEV, generator=g)
+    q = torch.zeros(T, Hq, 8, device=DEV)
+    q[:, ::7] = 0.5
+    out = torch.full((T, Hq, 8), 7.0, device=DEV)
+    batch = B.make_kv_batch(S, T, n, n, i32([0] * S), cu_tokens=i32(range(0, T + 1, n)))
+    B.np_attn_prompt(shape, 0, batch, i32(range(S * M)), q, pool, 0.3, 1, out, ws)
+    assert B.np_device_error(ws) == 0
+    values = pool[0, :, 1, 0].reshape(S, M * P, 8)[:, :n].reshape(T, 1, 8)
+    for t in range(0, T, 16384):
+        assert (out[t:t + 16384] == values[t:t + 16384]).all(), t
+    del q, out, pool
+    torch.cuda.empty_cache()

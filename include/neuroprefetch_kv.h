@@ -103,7 +103,8 @@ typedef struct np_kv_batch {
  * starts at q + t * q_stride + i * D (strides in elements, multiples of 8 for
  * 16-bit types and 4 for fp32, so views of one fused projection can be
  * given).  q_out receives the rotated queries (it may be q itself, with the
- * same stride; no other overlap). */
+ * same stride; no other overlap).  Of a batch without tokens (here and in the
+ * attention calls) the arrays may be NULL; such a call enqueues nothing. */
 typedef struct np_kv_rows {
   const void* q;
   const void* k;

@@ -61,10 +61,11 @@ static np_status check_batch(const char* fn, const np_kv_shape* s, int32_t layer
   return NP_OK;
 }
 
-// token rows of `heads` heads: stride in elements
+// token rows of `heads` heads: stride in elements.  An array of no tokens may
+// be anywhere.
 static np_status check_rows(const char* fn, const char* what, const np_kv_shape* s, const void* p,
-                            int64_t stride, int heads) {
-  if (!aligned16(p))
+                            int64_t stride, int heads, int n_tokens) {
+  if (n_tokens > 0 && !aligned16(p))
     return fail(NP_ERR_INVALID_ARG, "%s: %s must be non-NULL and 16-byte aligned", fn, what);
   if (stride < (int64_t)heads * s->head_dim || stride % vec_elems(s->dtype) ||
       stride > ((int64_t)1 << 31))
@@ -80,14 +81,14 @@ static np_status attn_common(const char* fn, const np_kv_shape* s, int32_t layer
                              void* out, int64_t out_stride, void* ws, hipStream_t stream) {
   np_status st = check_kv_shape(s);
   if (st == NP_OK) st = check_batch(fn, s, layer, b);
-  if (st == NP_OK) st = check_rows(fn, "q", s, q, q_stride, s->heads);
-  if (st == NP_OK) st = check_rows(fn, "out", s, out, out_stride, s->heads);
+  if (st == NP_OK) st = check_rows(fn, "q", s, q, q_stride, s->heads, b->n_tokens);
+  if (st == NP_OK) st = check_rows(fn, "out", s, out, out_stride, s->heads, b->n_tokens);
   if (st != NP_OK) return st;
   if (!std::isfinite(scale)) return fail(NP_ERR_INVALID_ARG, "%s: scale is not finite", fn);
   if (window < 0) return fail(NP_ERR_INVALID_ARG, "%s: window %d < 0", fn, window);
   if (!aligned16(table) || !aligned16(pool) || !aligned16(ws))
     return fail(NP_ERR_INVALID_ARG, "%s: pointers must be non-NULL and 16-byte aligned", fn);
-  if (out == q && out_stride != q_stride)
+  if (out == q && b->n_tokens > 0 && out_stride != q_stride)
     return fail(NP_ERR_INVALID_ARG, "%s: in place, but out_stride differs from q_stride", fn);
   if (b->n_seq == 0 || b->n_tokens == 0) return NP_OK;
   hipError_t e = launch_attn(*s, layer, *b, table, q, q_stride, pool, scale, window, out,
@@ -186,12 +187,13 @@ np_status np_kv_append(const np_kv_shape* s, int32_t layer, const np_kv_batch* b
   if (st == NP_OK) st = check_batch(fn, s, layer, b);
   if (st != NP_OK) return st;
   if (!r) return fail(NP_ERR_INVALID_ARG, "%s: rows is NULL", fn);
-  if ((st = check_rows(fn, "q", s, r->q, r->q_stride, s->heads)) != NP_OK ||
-      (st = check_rows(fn, "k", s, r->k, r->k_stride, s->kv_heads)) != NP_OK ||
-      (st = check_rows(fn, "v", s, r->v, r->v_stride, s->kv_heads)) != NP_OK ||
-      (st = check_rows(fn, "q_out", s, r->q_out, r->q_out_stride, s->heads)) != NP_OK)
+  const int n = b->n_tokens;
+  if ((st = check_rows(fn, "q", s, r->q, r->q_stride, s->heads, n)) != NP_OK ||
+      (st = check_rows(fn, "k", s, r->k, r->k_stride, s->kv_heads, n)) != NP_OK ||
+      (st = check_rows(fn, "v", s, r->v, r->v_stride, s->kv_heads, n)) != NP_OK ||
+      (st = check_rows(fn, "q_out", s, r->q_out, r->q_out_stride, s->heads, n)) != NP_OK)
     return st;
-  if (r->q_out == r->q && r->q_out_stride != r->q_stride)
+  if (r->q_out == r->q && n > 0 && r->q_out_stride != r->q_stride)
     return fail(NP_ERR_INVALID_ARG, "%s: in place, but q_out_stride differs from q_stride", fn);
   if (rot) {
     if (rot->dim < 16 || rot->dim % 16 || rot->dim > s->head_dim)

@@ -126,7 +126,7 @@ class KVCache:
             if n_new is None:
                 return B.make_kv_batch(n, n, 1, most, pos0, seqs=seqs)
             cu = self._ids(np.concatenate([[0], np.cumsum(n_new)]).tolist())
-            return B.make_kv_batch(n, sum(n_new), max(n_new), most, pos0, seqs=seqs, cu_tokens=cu)
+            return B.make_kv_batch(n, sum(n_new), max(n_new, default=0), most, pos0, seqs=seqs, cu_tokens=cu)
 
     def fork(self, src, dst, lens=None) -> None:
         with self.on_stream():
@@ -223,12 +223,12 @@ class DecoderLayers:
     def _layers(self, x, batch):
         hq, hk, hd = self.heads, self.kv_heads, self.head_dim
         for layer in range(self.cfg.layers):
-            qkv = (self._norm(x) @ self.wqkv[layer]).view(-1, hq + 2 * hk, hd)
+            qkv = (self._norm(x) @ self.wqkv[layer]).view(x.shape[0], hq + 2 * hk, hd)
             q = torch.empty(x.shape[0], hq, hd, dtype=x.dtype, device=self.device)
             out = torch.empty_like(q)
             self.cache.append(layer, batch, qkv[:, :hq], qkv[:, hq:hq + hk], qkv[:, hq + hk:], q)
             self.cache.attend(layer, batch, q, out, self.window)
-            x = x + out.view(-1, hq * hd) @ self.wo[layer]
+            x = x + out.view(x.shape[0], hq * hd) @ self.wo[layer]
             x = x + self._mlp(layer, self._norm(x))
         return x
 

@@ -448,18 +448,21 @@ __global__ __launch_bounds__(APP_T) void kv_append_kernel(AppendArgs a) {
   // include it, bad rows (reported with token 0) having none
   int row = t;
   if (a.b.cu) {
+    if (t == 0)
+      for (int i = threadIdx.x; i < a.b.n_seq; i += APP_T) {
+        const int lo = a.b.cu[i], hi = a.b.cu[i + 1];
+        if (lo < 0 || hi < lo || hi > a.b.n_tokens) raise(a.err, NP_DEVERR_STATE);
+      }
     row = -1;
     const int lane = threadIdx.x % WAVE;
-    for (int base = 0; base < a.b.n_seq && (row < 0 || t == 0); base += WAVE) {
-      bool mine = false;
-      if (base + lane < a.b.n_seq) {
-        const int lo = a.b.cu[base + lane], hi = a.b.cu[base + lane + 1];
-        const bool bad = lo < 0 || hi < lo || hi > a.b.n_tokens;
-        if (bad && t == 0 && threadIdx.x < WAVE) raise(a.err, NP_DEVERR_STATE);
-        mine = !bad && lo <= t && t < hi;
+    for (int base = 0; base < a.b.n_seq; base += WAVE) {
+      const int i = min(base + lane, a.b.n_seq - 1);
+      const int lo = a.b.cu[i], hi = a.b.cu[i + 1];
+      const uint64_t hit = __ballot((lo >= 0) & (lo <= t) & (t < hi) & (hi <= a.b.n_tokens));
+      if (hit) {
+        row = min(base + __ffsll((unsigned long long)hit) - 1, a.b.n_seq - 1);
+        break;
       }
-      const uint64_t hit = __ballot(mine);
-      if (hit && row < 0) row = base + __ffsll((unsigned long long)hit) - 1;
     }
     if (row < 0) return;  // nobody's token
   }

@@ -133,11 +133,12 @@ __device__ inline KvRow kv_row(const KvBatch& a, int b, int32_t* err) {
 // A grid of at least `blocks` workgroups of up to 256 threads, numbered by
 // grid_block().  A launch may have fewer than 2^32 threads along an axis; the
 // calls allow 2^24 tokens and 2^26 row blocks.
+constexpr int GRID_X = 23;  // log2 of the workgroups along x when there are several along y
 inline dim3 block_grid(int64_t blocks) {
-  const int64_t x = blocks < (1 << 23) ? blocks : 1 << 23;
+  const int64_t x = blocks < (1 << GRID_X) ? blocks : 1 << GRID_X;
   return dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
 }
-__device__ inline int grid_block() { return (int)(blockIdx.y * gridDim.x + blockIdx.x); }
+__device__ inline int grid_block() { return (int)(blockIdx.y << GRID_X | blockIdx.x); }
 
 // ---------------------------------------------------------------------------
 // launchers

@@ -88,7 +88,8 @@ typedef struct np_kv_state {
  * cu_tokens are bad has no tokens; a token that several others then claim is
  * appended for the first of them, and its outputs are those of any); a page
  * outside [0, N) where a token sees keys sets NP_DEVERR_NOT_RESIDENT (its keys
- * count as not visible).  At most 2^24 tokens and 2^30 query heads in all. */
+ * count as not visible).  Outputs of tokens that no row has are not written.  At
+ * most 2^24 tokens and 2^30 query heads in all. */
 typedef struct np_kv_batch {
   int32_t n_seq;
   int32_t n_tokens;

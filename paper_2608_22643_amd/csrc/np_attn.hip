@@ -209,8 +209,9 @@ __device__ inline float sum_groups(float v) {
 // 128, 537 MB in 95 us (5.65 TB/s; a plain stream of that length reaches 5.6 to
 // 6.1); 64 fp16 rows of 1 to 8192 keys, 326 MB in 69 us (4.7 TB/s).  Short calls
 // are bound by the chain table -> keys -> scores -> values -> join: 8.9 us for
-// 777 keys and 32 heads.  fp32 prompts run here too, bound by the fp32 matrix
-// cores.
+// 777 keys and 32 heads.  fp32 prompts run here too: 4096 tokens of 16 heads over
+// 4 at 81, 74 and 93 TFLOP/s for heads of 64, 128 and 256 (an 8192^3 fp32 library
+// product reaches 149 to 154).
 // ---------------------------------------------------------------------------
 constexpr int RB = 16;
 constexpr int NWAVE = 4;
@@ -752,10 +753,11 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(
 // cover the loads of the next; 64 keys, so that two workgroups fit a compute unit
 // and one's softmax runs beside the other's products.  No single part bounds it:
 // without the LDS reads of V 16384 bf16 tokens with 64 heads of 128 take 6% less,
-// without exponentials 5%, without loads 12%.  Those take 4.5 to 5.0 ms, 880 to
+// without exponentials 5%, without loads 12%; the matrix cores are busy 44% of the
+// time, LDS 33%, with no bank conflicts.  Those take 4.5 to 5.0 ms, 880 to
 // 980 TFLOP/s (an 8192^3 library product reaches 1140 to 1400, from card to card);
-// 2048 fp16 tokens and 32 heads 65 us (528 TFLOP/s; a library product of as many
-// operations 52 to 57 us).
+// 2048 fp16 tokens and 32 heads 62 to 65 us (530 to 550 TFLOP/s; a library product
+// of as many operations 52 to 57 us).
 // Measured and dropped: one workgroup of eight waves in two groups half a step
 // apart, 4.68 to 5.05 ms; the next step's score products dealt between this step's
 // exponentials, 4.56 ms (16384 tokens) and 119 against 106 us (packed prompts).

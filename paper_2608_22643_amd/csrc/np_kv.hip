@@ -436,8 +436,9 @@ constexpr int APP_T = 256;
 // takes units tid, tid + 256, ...  Everything is read once and written once,
 // so memory bounds it: four bf16 prompts of 9,800 tokens in all, 64 + 8 + 8
 // heads of 128, 483 MB in 90 us (5.4 TB/s; a large copy reaches 4.96).  With
-// few tokens the latency of cu_tokens -> row -> page -> heads does: 4.2 us for
-// 8 tokens, about 2 of them an empty launch.
+// few tokens the latency of position -> page -> heads does, in line as the code
+// has them (only the stores of keys and values need the page): 4.2 us for 8
+// tokens, about 2 of them an empty launch.
 template <class T, bool INTER>
 __global__ __launch_bounds__(APP_T) void kv_append_kernel(AppendArgs a) {
   constexpr int V = T::V;

@@ -115,6 +115,10 @@ class KVCache:
         list, since the host needs their sum); returns the step's batch for
         append, prompt and decode.  max_len: a bound on the lengths after the
         step, if the caller knows one."""
+        if n_new is not None:
+            n_new = [int(k) for k in n_new]
+            if any(k < 0 for k in n_new):
+                raise ValueError(f"negative token counts in {n_new}")
         with self.on_stream():
             seqs = self._ids(seqs)
             n = seqs.numel()

@@ -148,7 +148,56 @@ def test_lists_are_checked():
         for call in (lambda: c.extend(bad), lambda: c.fork(bad, [2, 3]), lambda: c.free(bad)):
             with pytest.raises(ValueError):
                 call()
-    for call in (lambda: c.extend([0, 1], [3]), lambda: c.fork([0, 1], [2]), lambda: c.fork([0], [1], [1, 1])):
+    for call in (lambda: c.extend([0, 1], [3]), lambda: c.extend([0, 1], [-2, 5]), lambda: c.fork([0, 1], [2]), lambda: c.fork([0], [1], [1, 1])):
         with pytest.raises(ValueError):
             call()
     assert c.pages_used() == 0 and c.device_error() == 0
+    for counts in (torch.tensor([17, 2]), torch.tensor([17, 2], device=DEV), (17, 2)):
+        batch = c.extend([0, 1], counts)
+        assert (batch.n_tokens, batch.max_tokens) == (19, 17)
+        c.free([0, 1])
+    assert c.device_error() == 0
+
+
+@pytest.mark.parametrize("beside", [False, True])
+def test_a_captured_step_follows_the_cache(beside):
+    """extend, append and attend of device lists captured on the cache's
+    stream, or on another one, and replayed with eager work between: the
+    outputs of an eager twin."""
+    stream = torch.cuda.Stream()
+    given = torch.cuda.Stream() if beside else stream
+    g = torch.Generator().manual_seed(5)
+    data = torch.randn(8, 3, 8, 64, generator=g).to(DEV)
+    outs = []
+    for captured in (False, True):
+        c = kvcache.KVCache(1, 4, 2, 64, "f32", 3, 64, 16, stream=given)
+        seqs = torch.tensor([2, 0, 1], dtype=torch.int32, device=DEV)
+        x, q, out = (torch.zeros(3, n, 64, device=DEV) for n in (8, 4, 4))
+
+        def step():
+            batch = c.extend(seqs)
+            c.append(0, batch, x[:, :4], x[:, 4:6], x[:, 6:], q)
+            c.attend(0, batch, q, out)
+
+        torch.cuda.synchronize()
+        if captured:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream, capture_error_mode="thread_local"):
+                step()
+            torch.cuda.synchronize()
+        got = []
+        for i in range(8):
+            x.copy_(data[i])
+            torch.cuda.synchronize()
+            if captured:
+                graph.replay()
+            else:
+                step()
+            torch.cuda.synchronize()
+            got.append(out.cpu())
+            scribble()
+            if i == 4:
+                c.free([0])
+        assert c.device_error() == 0 and c.kv_len.tolist() == [3, 8, 8]
+        outs.append(torch.stack(got))
+    assert torch.equal(outs[0], outs[1])

@@ -13,9 +13,12 @@
  *   np_kv_extend    room for the step's new tokens in every sequence: pages
  *                   from the free ones; a shared last page is copied first
  *   np_kv_append    rotary positions on the new queries and keys; keys and
- *                   values into their pages
+ *                   values into their pages (np_kv_append_norm: a norm of each
+ *                   query and key head before that)
  *   np_attn_decode  attention of one new token per sequence
+ *                   (np_attn_decode_shared: of sequences that share a prefix)
  *   np_attn_prompt  causal attention of many new tokens per sequence, packed
+ *   np_kv_read      tokens' keys and values back out of their pages
  *
  * and between steps np_kv_fork (a sequence that shares a prefix of another),
  * np_kv_free (a finished sequence) and np_kv_compact (the pages in use moved
@@ -26,14 +29,28 @@
  *  L = layers, Hq = heads, Hkv = kv_heads (query head i reads key-value head
  *  i / (Hq / Hkv)), D = head_dim, P = page_size (tokens a page holds),
  *  N = n_pages, S = max_seqs, M = seq_pages (pages a sequence can have),
- *  w = dtype of queries, keys, values and outputs.
+ *  w = dtype of queries, keys, values and outputs, plus NP_KV_E4M3 for a cache
+ *  of 8-bit elements.
  *  Requirements: L >= 1; Hkv divides Hq <= 1024; D a multiple of 8, 8..256;
  *  P one of 16, 32, 64, 128, 256; 1 <= N <= 2^20; 1 <= S <= 4096; M >= 1 and
- *  M * P <= 2^30.  Any violation is NP_ERR_INVALID_ARG.
+ *  M * P <= 2^30; with NP_KV_E4M3, D a multiple of 16.  Any violation is
+ *  NP_ERR_INVALID_ARG.
  *
  *  pool [L][N][2][Hkv][P][D] of type w, device: page p of layer l holds the
  *  keys ([0]) and the values ([1]) of P consecutive positions of a sequence,
  *  head by head.  The pool and one layer of it may be larger than 4 GiB.
+ *  With NP_KV_E4M3 the pool is bytes [L][N][2][Hkv][P D + P]: of each head, P
+ *  rows of D elements (OCP e4m3: 4 exponent and 3 mantissa bits, 448 the
+ *  largest, no infinities), then a byte b for each row, whose elements x stand
+ *  for x 2^(b - 127).  What is appended is first rounded to w, as for a plain
+ *  cache; a row whose largest finite magnitude is m then takes the least b >= 1
+ *  with m <= 448 2^(b - 127), and each value the nearest element, the even one
+ *  of two as near, except that the elements stop at 240 where 256 2^(b - 127)
+ *  is past the largest number of w.  A value that is not finite becomes NaN.  An
+ *  element is off by at most 2^-4 of its value, or 2^(b - 137) where that is
+ *  more (and by 1/16 of w's largest number, next to it).  All calls here take
+ *  such a cache; in place of w's values the attention calls see what the
+ *  elements stand for, which w holds exactly.
  *  np_kv_state, device int32: page_table [S][M] (page of positions
  *  [j P, (j+1) P) of sequence s, or -1), kv_len [S] (tokens reserved), refs
  *  [N] (how many sequences hold a page; 0: free).  np_kv_append and the
@@ -59,6 +76,9 @@
 extern "C" {
 #endif
 
+/* np_kv_shape.dtype: w, or w | NP_KV_E4M3 */
+#define NP_KV_E4M3 0x100
+
 typedef struct np_kv_shape {
   int32_t layers;    /* L */
   int32_t heads;     /* Hq */
@@ -68,7 +88,7 @@ typedef struct np_kv_shape {
   int32_t n_pages;   /* N */
   int32_t max_seqs;  /* S */
   int32_t seq_pages; /* M */
-  int32_t dtype;     /* np_dtype */
+  int32_t dtype;     /* np_dtype, | NP_KV_E4M3 for 8-bit elements */
 } np_kv_shape;
 
 typedef struct np_kv_state {
@@ -130,6 +150,33 @@ typedef struct np_rotary {
   int32_t max_pos;
   int32_t interleaved;
 } np_rotary;
+
+/* Norms of the query and key heads: q_weight and k_weight, device, type w, [D],
+ * 16-byte aligned, each NULL for ones; a head x becomes
+ *     x_d weight_d / sqrt(mean of x_d^2 over the head + eps)    (fp32).
+ * eps: finite, >= 0.  (A head of zeros stays zero, also when eps is 0.) */
+typedef struct np_qk_norm {
+  const void* q_weight;
+  const void* k_weight;
+  float eps;
+} np_qk_norm;
+
+/* Rows of a batch that share a prefix (np_attn_decode_shared): lead and prefix,
+ * device int32 [n_seq], 4-byte aligned.  lead[b] is the first row of row b's
+ * group: the rows of a group lie next to each other and all name the first of
+ * them, which names itself.  Sequence seqs[b] then has the same keys and values
+ * at positions 0 .. prefix[lead[b]] - 1 as sequence seqs[lead[b]] (as np_kv_fork
+ * makes them: the same pages, and copies of a partly filled last one); those of
+ * the latter are read.  prefix of other rows is not read.  max_prefix: a host
+ * value that no group's prefix exceeds.  A lead outside [0, b], one that does not
+ * name itself, whose rows do not lie next to each other, whose sequence is outside
+ * [0, S), or whose prefix is outside [0, max_prefix] sets NP_DEVERR_STATE, and the
+ * row is computed by itself, from its own pages, as in np_attn_decode. */
+typedef struct np_kv_shared {
+  int32_t max_prefix;
+  const int32_t* lead;
+  const int32_t* prefix;
+} np_kv_shared;
 
 /* Validates a shape (the requirements above).  Host only. */
 np_status np_kv_shape_check(const np_kv_shape* shape);
@@ -199,6 +246,23 @@ np_status np_kv_append(const np_kv_shape* shape, int32_t layer, const np_kv_batc
                        const int32_t* page_table, const np_kv_rows* rows,
                        const np_rotary* rotary, void* pool, void* dev_ws, hipStream_t stream);
 
+/* The same behind a norm of each query and key head (norm NULL: none), all in
+ * 32 bits up to the one rounding to w.  q_out, strides and what is not served as
+ * above.  One kernel. */
+np_status np_kv_append_norm(const np_kv_shape* shape, int32_t layer, const np_kv_batch* batch,
+                            const int32_t* page_table, const np_kv_rows* rows,
+                            const np_qk_norm* norm, const np_rotary* rotary, void* pool,
+                            void* dev_ws, hipStream_t stream);
+
+/* The batch's tokens read back from one layer: token t's keys of head i to k_out
+ * + t * k_stride + i * D, its values to v_out + t * v_stride + i * D (device, type
+ * w, strides in elements as in np_kv_rows; either may be NULL).  Zeros for tokens
+ * of a row that is not served, and, with NP_DEVERR_NOT_RESIDENT, where the table
+ * names no page; a token that no row has is not written.  One kernel. */
+np_status np_kv_read(const np_kv_shape* shape, int32_t layer, const np_kv_batch* batch,
+                     const int32_t* page_table, const void* pool, void* k_out, int64_t k_stride,
+                     void* v_out, int64_t v_stride, void* dev_ws, hipStream_t stream);
+
 /* Attention of the batch's tokens over the cache of one layer:
  *     out = sum_j softmax_j(scale q.k_j) v_j   over the keys the token sees,
  * zero where it sees none.  q and out: device, type w, head i of token t at
@@ -225,6 +289,19 @@ np_status np_attn_prompt(const np_kv_shape* shape, int32_t layer, const np_kv_ba
                          const int32_t* page_table, const void* q, int64_t q_stride,
                          const void* pool, float scale, int32_t window, void* out,
                          int64_t out_stride, void* dev_ws, hipStream_t stream);
+
+/* np_attn_decode for rows that share prefixes: the same outputs (up to the
+ * rounding of sums in another order; the same bits from run to run), but the
+ * keys and values of a group's prefix are read once for its rows together, each
+ * row's other keys after that.  Two kernels, the second to join the parts; where
+ * nothing can be gained (max_prefix 0; a batch of more than 32768 query heads in
+ * all; more than 128 query heads per key-value head, 16 in fp32) it is
+ * np_attn_decode, leads and prefixes then unread. */
+np_status np_attn_decode_shared(const np_kv_shape* shape, int32_t layer, const np_kv_batch* batch,
+                                const np_kv_shared* shared, const int32_t* page_table,
+                                const void* q, int64_t q_stride, const void* pool, float scale,
+                                int32_t window, void* out, int64_t out_stride, void* dev_ws,
+                                hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -19,7 +19,7 @@ ARCH = "gfx950"
 
 SOURCES = ["np_abi.cpp", "np_stage_host.cpp", "np_file.cpp", "np_predict.hip", "np_select.hip",
            "np_stage.hip", "np_mlp.hip", "np_calib.hip", "np_kv_abi.cpp", "np_kv.hip",
-           "np_attn.hip"]
+           "np_attn.hip", "np_attn8.hip", "np_attn_shared.hip"]
 
 FLAGS = ["-O3", "-fPIC", "-std=c++17", f"--offload-arch={ARCH}", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -18,6 +18,8 @@ LIB_PATH = os.path.join(_HERE, "libneuroprefetch.so")
  NP_ERR_IO) = range(7)
 NP_F32, NP_F16, NP_BF16 = 0, 1, 2
 DTYPE_CODE = {"f32": NP_F32, "f16": NP_F16, "bf16": NP_BF16}
+NP_KV_E4M3 = 0x100  # np_kv_shape.dtype: a cache of 8-bit elements
+CACHE_CODE = {None: 0, "same": 0, "e4m3": NP_KV_E4M3}
 NP_ACT_RELU, NP_ACT_SWIGLU = 0, 1
 ACT_CODE = {"relu": NP_ACT_RELU, "swiglu": NP_ACT_SWIGLU}
 NP_DEVERR_NAN_SCORE = 0x1
@@ -38,7 +40,7 @@ EXPORTS = ("np_status_str", "np_last_error", "np_shape_check", "np_workspace_siz
 # every symbol neuroprefetch_kv.h declares
 KV_EXPORTS = ("np_kv_shape_check", "np_kv_workspace_size", "np_kv_reset", "np_kv_extend",
               "np_kv_fork", "np_kv_free", "np_kv_compact", "np_kv_append", "np_attn_decode",
-              "np_attn_prompt")
+              "np_attn_prompt", "np_kv_append_norm", "np_kv_read", "np_attn_decode_shared")
 
 
 class NPError(RuntimeError):
@@ -102,6 +104,16 @@ class np_rotary(ctypes.Structure):
                 ("max_pos", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
 
 
+class np_qk_norm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("eps", ctypes.c_float)]
+
+
+class np_kv_shared(ctypes.Structure):
+    _fields_ = [("max_prefix", ctypes.c_int32), ("lead", ctypes.c_void_p),
+                ("prefix", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -163,6 +175,12 @@ def lib():
         L.np_attn_decode.argtypes = [K, i32, KB, vp, vp, i64, vp, ctypes.c_float, i32, vp, i64, vp,
                                      vp]
         L.np_attn_prompt.argtypes = L.np_attn_decode.argtypes
+        L.np_kv_append_norm.argtypes = [K, i32, KB, vp, ctypes.POINTER(np_kv_rows),
+                                        ctypes.POINTER(np_qk_norm), ctypes.POINTER(np_rotary), vp,
+                                        vp, vp]
+        L.np_kv_read.argtypes = [K, i32, KB, vp, vp, vp, i64, vp, i64, vp, vp]
+        L.np_attn_decode_shared.argtypes = [K, i32, KB, ctypes.POINTER(np_kv_shared), vp, vp, i64,
+                                            vp, ctypes.c_float, i32, vp, i64, vp, vp]
         for f in EXPORTS[2:] + KV_EXPORTS:
             getattr(L, f).restype = i32
         _lib = L
@@ -398,9 +416,19 @@ def _kept(s: ctypes.Structure, *tensors):
 
 
 def make_kv_shape(layers, heads, kv_heads, head_dim, page_size, n_pages, max_seqs, seq_pages,
-                  dtype) -> np_kv_shape:
+                  dtype, cache=None) -> np_kv_shape:
+    """cache: None or "same" (elements of dtype), or "e4m3" (8-bit elements)."""
+    if cache not in CACHE_CODE:
+        raise ValueError(f"cache {cache!r} is not one of {[c for c in CACHE_CODE if c]}")
     return np_kv_shape(layers, heads, kv_heads, head_dim, page_size, n_pages, max_seqs, seq_pages,
-                       DTYPE_CODE.get(dtype, dtype))
+                       DTYPE_CODE.get(dtype, dtype) | CACHE_CODE[cache])
+
+
+def kv_pool_shape(shape: np_kv_shape) -> tuple[int, ...]:
+    """Dimensions of a pool of np_kv_shape: of the type of the heads, or of bytes (e4m3)."""
+    row = ((shape.page_size * (shape.head_dim + 1),) if shape.dtype & NP_KV_E4M3
+           else (shape.page_size, shape.head_dim))
+    return (shape.layers, shape.n_pages, 2, shape.kv_heads) + row
 
 
 def make_kv_state(page_table, kv_len, refs) -> np_kv_state:
@@ -432,6 +460,22 @@ def make_rotary(cos, sin, interleaved: bool = False) -> np_rotary:
         raise ValueError("cos and sin: contiguous [max_pos][dim / 2] tensors of one shape")
     return _kept(np_rotary(_p(cos), _p(sin), 2 * cos.shape[1], cos.shape[0], int(interleaved)),
                  cos, sin)
+
+
+def make_qk_norm(q_weight=None, k_weight=None, eps: float = 1e-6) -> np_qk_norm:
+    """Weights: contiguous [head_dim] tensors of the heads' type, or None for ones."""
+    for w in (q_weight, k_weight):
+        if w is not None and (w.dim() != 1 or not w.is_contiguous()):
+            raise ValueError("weights: contiguous [head_dim] tensors")
+    return _kept(np_qk_norm(_p(q_weight), _p(k_weight), float(eps)), q_weight, k_weight)
+
+
+def make_kv_shared(lead, prefix, max_prefix: int) -> np_kv_shared:
+    """lead and prefix: int32 [n_seq] on the device, contiguous."""
+    for x in (lead, prefix):
+        if hasattr(x, "is_contiguous") and not x.is_contiguous():
+            raise ValueError("lead and prefix: contiguous [n_seq] tensors")
+    return _kept(np_kv_shared(int(max_prefix), _p(lead), _p(prefix)), lead, prefix)
 
 
 def np_kv_shape_check(shape: np_kv_shape) -> None:
@@ -477,6 +521,24 @@ def np_kv_append(shape, layer: int, batch: np_kv_batch, page_table, rows: np_kv_
                               _p(pool), _p(ws), _s(stream)), "np_kv_append")
 
 
+def np_kv_append_norm(shape, layer: int, batch: np_kv_batch, page_table, rows: np_kv_rows, norm,
+                      rotary, pool, ws, stream=None) -> None:
+    _check(lib().np_kv_append_norm(ctypes.byref(shape), int(layer), ctypes.byref(batch),
+                                   _p(page_table), ctypes.byref(rows),
+                                   None if norm is None else ctypes.byref(norm),
+                                   None if rotary is None else ctypes.byref(rotary), _p(pool),
+                                   _p(ws), _s(stream)), "np_kv_append_norm")
+
+
+def np_kv_read(shape, layer: int, batch: np_kv_batch, page_table, pool, k_out, v_out, ws,
+               stream=None) -> None:
+    """k_out and v_out: [tokens][kv_heads][head_dim] tensors, or None."""
+    ks, vs = (0 if x is None else _token_stride(x) for x in (k_out, v_out))
+    _check(lib().np_kv_read(ctypes.byref(shape), int(layer), ctypes.byref(batch), _p(page_table),
+                            _p(pool), _p(k_out), ks, _p(v_out), vs, _p(ws), _s(stream)),
+           "np_kv_read")
+
+
 def np_attn_decode(shape, layer: int, batch: np_kv_batch, page_table, q, pool, scale: float,
                    window: int, out, ws, stream=None) -> None:
     """q and out: [tokens][heads][head_dim] tensors."""
@@ -493,6 +555,16 @@ def np_attn_prompt(shape, layer: int, batch: np_kv_batch, page_table, q, pool, s
                                 _p(page_table), _p(q), _token_stride(q), _p(pool), float(scale),
                                 int(window), _p(out), _token_stride(out), _p(ws), _s(stream)),
            "np_attn_prompt")
+
+
+def np_attn_decode_shared(shape, layer: int, batch: np_kv_batch, shared: np_kv_shared, page_table, q,
+                          pool, scale: float, window: int, out, ws, stream=None) -> None:
+    """q and out: [tokens][heads][head_dim] tensors."""
+    _check(lib().np_attn_decode_shared(ctypes.byref(shape), int(layer), ctypes.byref(batch),
+                                       ctypes.byref(shared), _p(page_table), _p(q),
+                                       _token_stride(q), _p(pool), float(scale), int(window),
+                                       _p(out), _token_stride(out), _p(ws), _s(stream)),
+           "np_attn_decode_shared")
 
 
 def _ev(e) -> int | None:

@@ -14,6 +14,7 @@
 #include <limits.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "np_kv.hpp"
 
@@ -350,8 +351,9 @@ struct CopyArgs {
   char* pool;
   size_t layer_bytes, page_bytes;
   int blocks;       // 2 Hkv: blocks of a page of one layer
-  int block_bytes;  // P D w
+  int block_bytes;  // P D w, and the scales' P
   int row_bytes;    // D w
+  int scales_at;    // 8-bit elements: where a block's scales begin; 0: it has none
   int layers;
   int32_t* table;  // nullptr: no renaming
   size_t entries;
@@ -386,6 +388,8 @@ __global__ __launch_bounds__(COPY_T) void kv_copy_kernel(CopyArgs a) {
     const char* src = a.pool + at + (size_t)a.k.src[c] * a.page_bytes;
     char* dst = a.pool + at + (size_t)a.k.dst[c] * a.page_bytes;
     const int bytes = a.k.rows[c] * a.row_bytes;
+    if (a.scales_at)
+      for (int o = lane; o < a.k.rows[c]; o += WAVE) dst[a.scales_at + o] = src[a.scales_at + o];
     for (int o = lane * 16; o < bytes; o += WAVE * 16 * COPY_UNROLL) {
       uint4 v[COPY_UNROLL];
 #pragma unroll
@@ -413,6 +417,13 @@ struct AppendArgs {
   int Hq, Hkv, D, P, M, N;
   int R, max_pos;
   int32_t* err;
+  // norms and 8-bit elements (kv_append_heads_kernel)
+  bool norm;
+  const char *wq, *wk;  // nullptr: ones
+  float eps;
+  int lanes;  // log2 of the lanes that share a head
+  int parts;  // workgroups of a token
+  int top;    // the scale byte at which 256 2^(b - 127) leaves the type
 };
 
 template <class T>
@@ -431,6 +442,50 @@ __device__ inline uint4 pack_row(const float* f) {
 
 constexpr int APP_T = 256;
 
+// The place of token t in the cache.  Every thread of a workgroup takes part.
+// error: nullptr where another workgroup of the token reports.
+struct TokenAt {
+  enum { NOBODYS, UNSERVED, NO_PAGE, HERE } what;
+  int pos, page;
+};
+__device__ inline TokenAt find_token(const KvBatch& b, const int32_t* table, int M, int N, int P,
+                                     int t, int32_t* error) {
+  // the token's row, as the attention calls have it: the one whose tokens
+  // include it, bad rows (reported with token 0) having none
+  int row = t;
+  if (b.cu) {
+    if (t == 0 && error)
+      for (int i = threadIdx.x; i < b.n_seq; i += APP_T) {
+        const int lo = b.cu[i], hi = b.cu[i + 1];
+        if (lo < 0 || hi < lo || hi > b.n_tokens) raise(error, NP_DEVERR_STATE);
+      }
+    row = -1;
+    const int lane = threadIdx.x % WAVE;
+    for (int base = 0; base < b.n_seq; base += WAVE) {
+      const int i = min(base + lane, b.n_seq - 1);
+      const int lo = b.cu[i], hi = b.cu[i + 1];
+      const uint64_t hit = __ballot((lo >= 0) & (lo <= t) & (t < hi) & (hi <= b.n_tokens));
+      if (hit) {
+        row = min(base + __ffsll((unsigned long long)hit) - 1, b.n_seq - 1);
+        break;
+      }
+    }
+    if (row < 0) return {TokenAt::NOBODYS, -1, -1};
+  }
+  row = __builtin_amdgcn_readfirstlane(row);
+  int32_t* err = threadIdx.x == 0 ? error : nullptr;
+  const KvRow r = kv_row(b, row, err);
+  if (t < r.begin || t >= r.begin + r.n) return {TokenAt::NOBODYS, -1, -1};
+  if (r.p0 < 0) return {TokenAt::UNSERVED, -1, -1};
+  const int pos = r.p0 + (t - r.begin);
+  const int page = table[(size_t)r.seq * M + pos / P];
+  if (page < 0 || page >= N) {
+    if (err) raise(err, NP_DEVERR_NOT_RESIDENT);
+    return {TokenAt::NO_PAGE, pos, -1};
+  }
+  return {TokenAt::HERE, pos, page};
+}
+
 // A workgroup per token.  A unit is 16 bytes of a head, or for the split pairs
 // (i, i + R/2) the two pieces of 16 bytes that turn into each other; a thread
 // takes units tid, tid + 256, ...  Everything is read once and written once,
@@ -445,40 +500,11 @@ __global__ __launch_bounds__(APP_T) void kv_append_kernel(AppendArgs a) {
   constexpr int W = 16 / V;
   const int t = grid_block();
   if (t >= a.b.n_tokens) return;
-  // the token's row, as the attention calls have it: the one whose tokens
-  // include it, bad rows (reported with token 0) having none
-  int row = t;
-  if (a.b.cu) {
-    if (t == 0)
-      for (int i = threadIdx.x; i < a.b.n_seq; i += APP_T) {
-        const int lo = a.b.cu[i], hi = a.b.cu[i + 1];
-        if (lo < 0 || hi < lo || hi > a.b.n_tokens) raise(a.err, NP_DEVERR_STATE);
-      }
-    row = -1;
-    const int lane = threadIdx.x % WAVE;
-    for (int base = 0; base < a.b.n_seq; base += WAVE) {
-      const int i = min(base + lane, a.b.n_seq - 1);
-      const int lo = a.b.cu[i], hi = a.b.cu[i + 1];
-      const uint64_t hit = __ballot((lo >= 0) & (lo <= t) & (t < hi) & (hi <= a.b.n_tokens));
-      if (hit) {
-        row = min(base + __ffsll((unsigned long long)hit) - 1, a.b.n_seq - 1);
-        break;
-      }
-    }
-    if (row < 0) return;  // nobody's token
-  }
-  row = __builtin_amdgcn_readfirstlane(row);
-  int32_t* err = threadIdx.x == 0 ? a.err : nullptr;
-  const KvRow r = kv_row(a.b, row, err);
-  if (r.p0 < 0 || t < r.begin || t >= r.begin + r.n) return;
-  const int pos = r.p0 + (t - r.begin);
-  const int page = a.table[(size_t)r.seq * a.M + pos / a.P];
-  if (page < 0 || page >= a.N) {
-    if (err) raise(err, NP_DEVERR_NOT_RESIDENT);
-    return;
-  }
+  const TokenAt at = find_token(a.b, a.table, a.M, a.N, a.P, t, a.err);
+  if (at.what != TokenAt::HERE) return;
+  const int pos = at.pos, page = at.page;
   if (a.R && pos >= a.max_pos) {
-    if (err) raise(err, NP_DEVERR_STATE);
+    if (threadIdx.x == 0) raise(a.err, NP_DEVERR_STATE);
     return;
   }
   const char* q = a.q + t * a.q_stride;
@@ -555,6 +581,271 @@ __global__ __launch_bounds__(APP_T) void kv_append_kernel(AppendArgs a) {
   }
 }
 
+// A reduction over 2^lanes neighbouring lanes, all of which get the result:
+// within 16 by moves between lanes' registers, past them by swapped rows.
+template <class Op>
+__device__ inline float reduce_lanes(float v, int lanes, Op op) {
+  auto dpp = [&](auto ctrl) {
+    const int x = __float_as_int(v);
+    return op(v, __int_as_float(__builtin_amdgcn_update_dpp(x, x, decltype(ctrl)::value, 0xF, 0xF,
+                                                            false)));
+  };
+  if (lanes > 0) v = dpp(std::integral_constant<int, 0xB1>{});   // lane ^ 1
+  if (lanes > 1) v = dpp(std::integral_constant<int, 0x4E>{});   // lane ^ 2
+  if (lanes > 2) v = dpp(std::integral_constant<int, 0x141>{});  // 7 - lane, within eight
+  if (lanes > 3) v = dpp(std::integral_constant<int, 0x140>{});  // 15 - lane, within sixteen
+  if (lanes > 4) {
+    const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                    false);
+    v = op(__uint_as_float(x[0]), __uint_as_float(x[1]));
+  }
+  if (lanes > 5) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                    false);
+    v = op(__uint_as_float(x[0]), __uint_as_float(x[1]));
+  }
+  return v;
+}
+
+__device__ inline bool finite_f32(float v) {
+  return (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u;
+}
+
+// The scale byte of a row with largest finite magnitude m: the least b >= 1
+// with m <= 448 2^(b - 127); 448 is 1.75 2^8.
+__device__ inline int scale_byte(float m) {
+  const uint32_t u = __float_as_uint(m);
+  return max(1, (int)(u >> 23) - 8 + ((u & 0x007FFFFFu) > 0x00600000u ? 1 : 0));
+}
+
+// V values as elements under scale byte b, rounded to the nearest (ties to
+// even); what is not finite becomes NaN.
+template <int V>
+__device__ inline void to_elements(const float* f, int b, int top, uint32_t* out) {
+  const float inv = scale_of_byte(254 - b), most = b >= top ? 240.f : 448.f;
+  float y[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e)
+    y[e] = finite_f32(f[e]) ? fminf(fmaxf(f[e] * inv, -most), most) : __uint_as_float(0x7FC00000u);
+#pragma unroll
+  for (int e = 0; e < V; e += 4) {
+    int x = __builtin_amdgcn_cvt_pk_fp8_f32(y[e], y[e + 1], 0, false);
+    out[e / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[e + 2], y[e + 3], x, true);
+  }
+}
+
+// np_kv_append_norm, and any append of 8-bit elements.  A head is shared by
+// 2^lanes neighbouring lanes, each with the unit of 16 or 2 x 16 bytes of
+// kv_append_kernel, so that the sum of squares and the largest magnitude are
+// reductions between lanes' registers; a workgroup has 256 >> lanes heads of a
+// token.  The heads are asked for before the token's place is looked up: their
+// addresses need only its number.
+template <class T, bool INTER, bool E8>
+__global__ __launch_bounds__(APP_T) void kv_append_heads_kernel(AppendArgs a) {
+  constexpr int V = T::V;
+  constexpr int W = 16 / V;
+  const int id = grid_block();
+  const int t = id / a.parts;
+  if (t >= a.b.n_tokens) return;
+  const int chunks = a.D / V;
+  const int half = INTER ? 0 : a.R / 2 / V;  // pieces that have a partner
+  const int u = threadIdx.x & ((1 << a.lanes) - 1);
+  int h = ((id % a.parts) << (__builtin_ctz(APP_T) - a.lanes)) + ((int)threadIdx.x >> a.lanes);
+  const int kind = h < a.Hq ? 0 : h < a.Hq + a.Hkv ? 1 : 2;
+  const bool live = h < a.Hq + 2 * a.Hkv && u < chunks - half;
+  if (kind) h -= a.Hq + (kind - 1) * a.Hkv;
+  const bool pair = u < half;
+  const int c0 = pair ? u : u + half, c1 = u + half;  // this lane's pieces, c1 only of pairs
+
+  uint4 xa = make_uint4(0, 0, 0, 0), xb = xa;
+  uint4 ga = xa, gb = xa;
+  const char* g = kind == 0 ? a.wq : kind == 1 ? a.wk : nullptr;
+  if (live) {
+    const char* src = kind == 0   ? a.q + t * a.q_stride
+                      : kind == 1 ? a.k + t * a.k_stride
+                                  : a.v + t * a.v_stride;
+    src += (size_t)h * a.D * W;
+    xa = *(const uint4*)(src + c0 * 16);
+    if (pair) xb = *(const uint4*)(src + c1 * 16);
+    if (g) {
+      ga = *(const uint4*)(g + c0 * 16);
+      if (pair) gb = *(const uint4*)(g + c1 * 16);
+    }
+  }
+
+  const TokenAt at = find_token(a.b, a.table, a.M, a.N, a.P, t, id % a.parts ? nullptr : a.err);
+  if (at.what != TokenAt::HERE) return;
+  if (a.R && at.pos >= a.max_pos) {
+    if (threadIdx.x == 0 && id % a.parts == 0) raise(a.err, NP_DEVERR_STATE);
+    return;
+  }
+
+  float f[2 * V];
+  T::unpack(xa, f);
+  T::unpack(xb, f + V);
+  if (a.norm) {
+    // the mean square in fp32; where the sum would leave fp32's range, that of
+    // the head divided by a power of two next to its largest magnitude (or to
+    // eps's root), which every lane of a head finds alike
+    float ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < 2 * V; ++e) ss = __builtin_fmaf(f[e], f[e], ss);
+    ss = reduce_lanes(ss, a.lanes, [](float x, float y) { return x + y; });
+    float mean = ss / (float)a.D + a.eps;
+    float r = mean > 0.f ? 1.f / sqrtf(mean) : 0.f;
+    float down = 1.f;
+    const bool far = !(ss < 1e36f) || mean < 1e-27f;
+    if (__any(kind < 2 && live && far)) {
+      float m = 0.f;
+#pragma unroll
+      for (int e = 0; e < 2 * V; ++e) m = finite_f32(f[e]) ? fmaxf(m, fabsf(f[e])) : m;
+      m = reduce_lanes(m, a.lanes, [](float x, float y) { return fmaxf(x, y); });
+      m = fmaxf(m, sqrtf(a.eps));
+      const int ex = min(max((int)(__float_as_uint(m) >> 23), 2), 252);
+      const float scale = scale_of_byte(254 - ex);
+      float s2 = 0.f;
+#pragma unroll
+      for (int e = 0; e < 2 * V; ++e) s2 = __builtin_fmaf(f[e] * scale, f[e] * scale, s2);
+      s2 = reduce_lanes(s2, a.lanes, [](float x, float y) { return x + y; });
+      if (far && m > 0.f) {
+        down = scale;
+        r = 1.f / sqrtf(s2 / (float)a.D + a.eps * scale * scale);
+      }
+    }
+    if (kind < 2) {
+      float w[2 * V];
+      T::unpack(ga, w);
+      T::unpack(gb, w + V);
+#pragma unroll
+      for (int e = 0; e < 2 * V; ++e) f[e] = f[e] * down * r * (g ? w[e] : 1.f);
+    }
+  }
+  const bool turned = kind < 2 && (INTER ? c0 * V < a.R : pair);
+  if (turned) {
+    const float* cs = a.cos + (size_t)at.pos * (a.R / 2);
+    const float* sn = a.sin + (size_t)at.pos * (a.R / 2);
+    float o[2 * V];
+    if constexpr (INTER) {
+#pragma unroll
+      for (int e = 0; e < V; e += 2) {
+        const float co = cs[(c0 * V + e) / 2], si = sn[(c0 * V + e) / 2];
+        o[e] = f[e] * co - f[e + 1] * si;
+        o[e + 1] = f[e + 1] * co + f[e] * si;
+        o[e + V] = o[e + V + 1] = 0.f;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; e += 4) {
+        const float4 co = *(const float4*)(cs + c0 * V + e), si = *(const float4*)(sn + c0 * V + e);
+        const float* cp = &co.x;
+        const float* sp = &si.x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          o[e + j] = f[e + j] * cp[j] - f[e + j + V] * sp[j];
+          o[e + j + V] = f[e + j + V] * cp[j] + f[e + j] * sp[j];
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 2 * V; ++e) f[e] = o[e];
+  }
+  if (kind < 2 && (a.norm || turned)) {  // the rounding to w
+    xa = pack_row<T>(f);
+    xb = pack_row<T>(f + V);
+  }
+  if (kind == 0 && live) {
+    char* dst = a.q_out + t * a.q_out_stride + (size_t)h * a.D * W;
+    *(uint4*)(dst + c0 * 16) = xa;
+    if (pair) *(uint4*)(dst + c1 * 16) = xb;
+  }
+  const int blk = (kind == 2 ? a.Hkv : 0) + h;  // of the page
+  const int slot = at.pos % a.P;
+  char* page = a.pool + (size_t)at.page * a.page_bytes;
+  if constexpr (!E8) {
+    if (!live || kind == 0) return;
+    char* dst = page + ((size_t)blk * a.P + slot) * a.D * W;
+    *(uint4*)(dst + c0 * 16) = xa;
+    if (pair) *(uint4*)(dst + c1 * 16) = xb;
+  } else {
+    // every lane takes part in the reduction, those of queries among them
+    T::unpack(xa, f);
+    T::unpack(xb, f + V);
+    float m = 0.f;
+#pragma unroll
+    for (int e = 0; e < 2 * V; ++e) m = finite_f32(f[e]) ? fmaxf(m, fabsf(f[e])) : m;
+    m = reduce_lanes(m, a.lanes, [](float x, float y) { return fmaxf(x, y); });
+    if (!live || kind == 0) return;
+    const int b = scale_byte(m);
+    char* dst = page + (size_t)blk * a.P * (a.D + 1);
+    uint32_t ea[V / 4], eb[V / 4];
+    to_elements<V>(f, b, a.top, ea);
+    to_elements<V>(f + V, b, a.top, eb);
+    auto put = [&](int c, const uint32_t* e) {
+      char* p = dst + slot * a.D + c * V;
+      if constexpr (V == 8) *(uint2*)p = make_uint2(e[0], e[1]);
+      else *(uint32_t*)p = e[0];
+    };
+    put(c0, ea);
+    if (pair) put(c1, eb);
+    if (u == 0) dst[a.P * a.D + slot] = (char)b;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// np_kv_read: pieces of 16 bytes of a token's keys and values, a thread each.
+// ---------------------------------------------------------------------------
+struct ReadArgs {
+  KvBatch b;
+  const int32_t* table;
+  const char* pool;  // of the layer
+  char *k, *v;
+  int64_t k_stride, v_stride;  // bytes
+  size_t page_bytes;
+  int Hkv, D, P, M, N, parts;
+  int32_t* err;
+};
+
+template <class T, bool E8>
+__global__ __launch_bounds__(APP_T) void kv_read_kernel(ReadArgs a) {
+  constexpr int V = T::V;
+  const int id = grid_block();
+  const int t = id / a.parts, part = id % a.parts;
+  if (t >= a.b.n_tokens) return;
+  const TokenAt at = find_token(a.b, a.table, a.M, a.N, a.P, t, part ? nullptr : a.err);
+  if (at.what == TokenAt::NOBODYS) return;
+  const int chunks = a.D / V, n = a.Hkv * chunks;
+  int c = part * APP_T + (int)threadIdx.x;
+  const bool value = c >= n;
+  if (value) c -= n;
+  char* out = value ? a.v : a.k;
+  if (c >= n || !out) return;
+  out += t * (value ? a.v_stride : a.k_stride) + (int64_t)c * 16;
+  uint4 x = make_uint4(0, 0, 0, 0);
+  if (at.what == TokenAt::HERE) {
+    const int h = c / chunks, slot = at.pos % a.P;
+    c -= h * chunks;
+    const char* page = a.pool + (size_t)at.page * a.page_bytes;
+    const int blk = (value ? a.Hkv : 0) + h;
+    if constexpr (!E8) {
+      x = *(const uint4*)(page + (((size_t)blk * a.P + slot) * a.D + c * V) * (16 / V));
+    } else {
+      const char* row = page + (size_t)blk * a.P * (a.D + 1);
+      const float s = scale_of_byte((uint8_t)row[a.P * a.D + slot]);
+      if constexpr (V == 8) {
+        const uint2 e = *(const uint2*)(row + slot * a.D + c * V);
+        x = make_uint4(element_pair<T>(e.x, s, false), element_pair<T>(e.x, s, true),
+                       element_pair<T>(e.y, s, false), element_pair<T>(e.y, s, true));
+      } else {
+        const f32x2_t lo = element_pair_f32(*(const uint32_t*)(row + slot * a.D + c * V), s, false);
+        const f32x2_t hi = element_pair_f32(*(const uint32_t*)(row + slot * a.D + c * V), s, true);
+        x = make_uint4(__float_as_uint(lo.x), __float_as_uint(lo.y), __float_as_uint(hi.x),
+                       __float_as_uint(hi.y));
+      }
+    }
+  }
+  *(uint4*)out = x;
+}
+
 }  // namespace
 
 // ---------------------------------------------------------------------------
@@ -582,8 +873,9 @@ static hipError_t launch_copies(const np_kv_shape& s, const KvScratch& k, void* 
   a.page_bytes = kv_page_bytes(s);
   a.layer_bytes = a.page_bytes * s.n_pages;
   a.blocks = 2 * s.kv_heads;
-  a.row_bytes = s.head_dim * dtype_size(s.dtype);
-  a.block_bytes = s.page_size * a.row_bytes;
+  a.row_bytes = kv_row_bytes(s);
+  a.block_bytes = s.page_size * (a.row_bytes + kv_scale_bytes(s));
+  a.scales_at = kv_e4m3(s) ? s.page_size * a.row_bytes : 0;
   a.layers = s.layers;
   a.table = table;
   a.entries = (size_t)s.max_seqs * s.seq_pages;
@@ -646,9 +938,10 @@ hipError_t launch_kv_compact(const np_kv_shape& s, const np_kv_state& st, void* 
 }
 
 hipError_t launch_kv_append(const np_kv_shape& s, int layer, const np_kv_batch& b,
-                            const int32_t* table, const np_kv_rows& r, const np_rotary* rot,
-                            void* pool, void* ws, hipStream_t stream) {
-  const int64_t w = dtype_size(s.dtype);
+                            const int32_t* table, const np_kv_rows& r, const np_qk_norm* norm,
+                            const np_rotary* rot, void* pool, void* ws, hipStream_t stream) {
+  const int dtype = kv_dtype(s);
+  const int64_t w = dtype_size(dtype);
   AppendArgs a;
   a.b = {b.seqs, b.cu_tokens, b.pos0, b.n_seq, b.n_tokens, s.max_seqs,
          (int)std::min<int64_t>(b.max_len, (int64_t)s.seq_pages * s.page_size)};
@@ -674,20 +967,70 @@ hipError_t launch_kv_append(const np_kv_shape& s, int layer, const np_kv_batch& 
   a.M = s.seq_pages;
   a.N = s.n_pages;
   a.err = (int32_t*)((char*)ws + WS_ERR);
-  const bool inter = rot && rot->interleaved;
-  auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, block_grid(b.n_tokens), dim3(APP_T), 0, stream, a);
+  const bool inter = rot && rot->interleaved, e8 = kv_e4m3(s);
+  const bool heads = norm || e8;
+  a.norm = norm;
+  a.wq = norm ? (const char*)norm->q_weight : nullptr;
+  a.wk = norm ? (const char*)norm->k_weight : nullptr;
+  a.eps = norm ? norm->eps : 0.f;
+  a.top = dtype == NP_F16 ? 127 + 8 : 127 + 120;
+  const int v = vec_elems(dtype), units = a.D / v - (inter ? 0 : a.R / 2 / v);
+  a.lanes = 0;
+  while (1 << a.lanes < units) ++a.lanes;
+  const int per = APP_T >> a.lanes;  // heads of a workgroup
+  a.parts = (s.heads + 2 * s.kv_heads + per - 1) / per;
+  auto go = [&](auto kernel, int64_t blocks) {
+    hipLaunchKernelGGL(kernel, block_grid(blocks), dim3(APP_T), 0, stream, a);
   };
-  if (s.dtype == NP_F32) {
-    if (inter) go(kv_append_kernel<TF32, true>);
-    else go(kv_append_kernel<TF32, false>);
-  } else if (s.dtype == NP_F16) {
-    if (inter) go(kv_append_kernel<TF16, true>);
-    else go(kv_append_kernel<TF16, false>);
-  } else {
-    if (inter) go(kv_append_kernel<TBF16, true>);
-    else go(kv_append_kernel<TBF16, false>);
-  }
+  auto of = [&](auto t) {
+    using T = decltype(t);
+    const int64_t n = b.n_tokens, parts = n * a.parts;
+    if (!heads) inter ? go(kv_append_kernel<T, true>, n) : go(kv_append_kernel<T, false>, n);
+    else if (e8) inter ? go(kv_append_heads_kernel<T, true, true>, parts)
+                       : go(kv_append_heads_kernel<T, false, true>, parts);
+    else inter ? go(kv_append_heads_kernel<T, true, false>, parts)
+               : go(kv_append_heads_kernel<T, false, false>, parts);
+  };
+  if (dtype == NP_F32) of(TF32{});
+  else if (dtype == NP_F16) of(TF16{});
+  else of(TBF16{});
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_read(const np_kv_shape& s, int layer, const np_kv_batch& b,
+                          const int32_t* table, const void* pool, void* k, int64_t k_stride,
+                          void* v, int64_t v_stride, void* ws, hipStream_t stream) {
+  const int dtype = kv_dtype(s);
+  const int64_t w = dtype_size(dtype);
+  ReadArgs a;
+  a.b = {b.seqs, b.cu_tokens, b.pos0, b.n_seq, b.n_tokens, s.max_seqs,
+         (int)std::min<int64_t>(b.max_len, (int64_t)s.seq_pages * s.page_size)};
+  a.table = table;
+  a.page_bytes = kv_page_bytes(s);
+  a.pool = (const char*)pool + (size_t)layer * s.n_pages * a.page_bytes;
+  a.k = (char*)k;
+  a.v = (char*)v;
+  a.k_stride = k_stride * w;
+  a.v_stride = v_stride * w;
+  a.Hkv = s.kv_heads;
+  a.D = s.head_dim;
+  a.P = s.page_size;
+  a.M = s.seq_pages;
+  a.N = s.n_pages;
+  a.parts = (2 * s.kv_heads * (s.head_dim / vec_elems(dtype)) + APP_T - 1) / APP_T;
+  a.err = (int32_t*)((char*)ws + WS_ERR);
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, block_grid((int64_t)b.n_tokens * a.parts), dim3(APP_T), 0, stream,
+                       a);
+  };
+  auto of = [&](auto t) {
+    using T = decltype(t);
+    if (kv_e4m3(s)) go(kv_read_kernel<T, true>);
+    else go(kv_read_kernel<T, false>);
+  };
+  if (dtype == NP_F32) of(TF32{});
+  else if (dtype == NP_F16) of(TF16{});
+  else of(TBF16{});
   return hipGetLastError();
 }
 

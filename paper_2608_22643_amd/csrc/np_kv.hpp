@@ -59,9 +59,16 @@ inline size_t kv_ws_layout(const np_kv_shape& s, char* ws, KvScratch* k) {
   return at;
 }
 
-// bytes of one page of one layer
+// The type of the heads, and whether the cache holds 8-bit elements.
+inline int kv_dtype(const np_kv_shape& s) { return s.dtype & ~NP_KV_E4M3; }
+inline bool kv_e4m3(const np_kv_shape& s) { return s.dtype & NP_KV_E4M3; }
+// bytes of a row of the cache, of its scale, and of one page of one layer
+inline int kv_row_bytes(const np_kv_shape& s) {
+  return s.head_dim * (kv_e4m3(s) ? 1 : dtype_size(s.dtype));
+}
+inline int kv_scale_bytes(const np_kv_shape& s) { return kv_e4m3(s) ? 1 : 0; }
 inline size_t kv_page_bytes(const np_kv_shape& s) {
-  return (size_t)2 * s.kv_heads * s.page_size * s.head_dim * dtype_size(s.dtype);
+  return (size_t)2 * s.kv_heads * s.page_size * (kv_row_bytes(s) + kv_scale_bytes(s));
 }
 
 // ---------------------------------------------------------------------------
@@ -130,6 +137,29 @@ __device__ inline KvRow kv_row(const KvBatch& a, int b, int32_t* err) {
   return kv_row_check(a, kv_row_load(a, b), err);
 }
 
+// 2^(b - 127) of a row's scale byte (1 .. 254)
+__device__ inline float scale_of_byte(uint32_t b) { return __uint_as_float(b << 23); }
+
+// Two elements (the low or the high half of a dword of four) times a scale that
+// is a power of two, as a dword of 16-bit values, or as two fp32.
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+template <class T>
+__device__ inline uint32_t element_pair(uint32_t e, float scale, bool high) {
+  if constexpr (T::dtype == NP_F16) {
+    const half2_t x = high ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(e, scale, true)
+                           : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(e, scale, false);
+    return __builtin_bit_cast(uint32_t, x);
+  } else {
+    const bf162_t x = high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(e, scale, true)
+                           : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(e, scale, false);
+    return __builtin_bit_cast(uint32_t, x);
+  }
+}
+__device__ inline f32x2_t element_pair_f32(uint32_t e, float scale, bool high) {
+  return high ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(e, scale, true)
+              : __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(e, scale, false);
+}
+
 // A grid of at least `blocks` workgroups of up to 256 threads, numbered by
 // grid_block().  A launch may have fewer than 2^32 threads along an axis; the
 // calls allow 2^24 tokens and 2^26 row blocks.
@@ -155,11 +185,18 @@ hipError_t launch_kv_free(const np_kv_shape& s, const np_kv_state& st, int n, co
 hipError_t launch_kv_compact(const np_kv_shape& s, const np_kv_state& st, void* pool,
                              int32_t* n_moved, void* ws, hipStream_t stream);
 hipError_t launch_kv_append(const np_kv_shape& s, int layer, const np_kv_batch& b,
-                            const int32_t* table, const np_kv_rows& r, const np_rotary* rot,
-                            void* pool, void* ws, hipStream_t stream);
+                            const int32_t* table, const np_kv_rows& r, const np_qk_norm* norm,
+                            const np_rotary* rot, void* pool, void* ws, hipStream_t stream);
+hipError_t launch_kv_read(const np_kv_shape& s, int layer, const np_kv_batch& b,
+                          const int32_t* table, const void* pool, void* k, int64_t k_stride,
+                          void* v, int64_t v_stride, void* ws, hipStream_t stream);
 hipError_t launch_attn(const np_kv_shape& s, int layer, const np_kv_batch& b,
                        const int32_t* table, const void* q, int64_t q_stride, const void* pool,
                        float scale, int window, void* out, int64_t out_stride, void* ws,
                        hipStream_t stream);
+hipError_t launch_attn_shared(const np_kv_shape& s, int layer, const np_kv_batch& b,
+                              const np_kv_shared& sh, const int32_t* table, const void* q,
+                              int64_t q_stride, const void* pool, float scale, int window,
+                              void* out, int64_t out_stride, void* ws, hipStream_t stream);
 
 }  // namespace np

@@ -8,18 +8,23 @@
 namespace np {
 
 static bool aligned4(const void* p) { return p && ((uintptr_t)p & 3u) == 0; }
+static bool aligned16_or_null(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 static bool aligned4_or_null(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 
 static np_status check_kv_shape(const np_kv_shape* s) {
   if (!s) return fail(NP_ERR_INVALID_ARG, "kv shape is NULL");
-  if (s->dtype < NP_F32 || s->dtype > NP_BF16)
-    return fail(NP_ERR_INVALID_ARG, "dtype %d is not an np_dtype", s->dtype);
+  if (kv_dtype(*s) < NP_F32 || kv_dtype(*s) > NP_BF16)
+    return fail(NP_ERR_INVALID_ARG, "dtype %d is not an np_dtype, nor one with NP_KV_E4M3",
+                s->dtype);
   if (s->layers < 1) return fail(NP_ERR_INVALID_ARG, "layers %d < 1", s->layers);
   if (s->heads < 1 || s->heads > 1024 || s->kv_heads < 1 || s->heads % s->kv_heads)
     return fail(NP_ERR_INVALID_ARG, "heads %d (at most 1024) and kv_heads %d: kv_heads must divide heads",
                 s->heads, s->kv_heads);
   if (s->head_dim < 8 || s->head_dim > 256 || s->head_dim % 8)
     return fail(NP_ERR_INVALID_ARG, "head_dim %d is not a multiple of 8 in [8, 256]", s->head_dim);
+  if (kv_e4m3(*s) && s->head_dim % 16)
+    return fail(NP_ERR_INVALID_ARG, "head_dim %d of a cache of 8-bit elements is not a multiple of 16",
+                s->head_dim);
   const int P = s->page_size;
   if (P < 16 || P > 256 || (P & (P - 1)))
     return fail(NP_ERR_INVALID_ARG, "page_size %d is not one of 16, 32, 64, 128, 256", P);
@@ -67,18 +72,57 @@ static np_status check_rows(const char* fn, const char* what, const np_kv_shape*
                             int64_t stride, int heads, int n_tokens) {
   if (n_tokens > 0 && !aligned16(p))
     return fail(NP_ERR_INVALID_ARG, "%s: %s must be non-NULL and 16-byte aligned", fn, what);
-  if (stride < (int64_t)heads * s->head_dim || stride % vec_elems(s->dtype) ||
+  if (stride < (int64_t)heads * s->head_dim || stride % vec_elems(kv_dtype(*s)) ||
       stride > ((int64_t)1 << 31))
     return fail(NP_ERR_INVALID_ARG,
                 "%s: %s stride %lld: a multiple of %d elements, at least a token's %d", fn, what,
-                (long long)stride, vec_elems(s->dtype), heads * s->head_dim);
+                (long long)stride, vec_elems(kv_dtype(*s)), heads * s->head_dim);
   return NP_OK;
 }
 
+static np_status append_common(const char* fn, const np_kv_shape* s, int32_t layer,
+                               const np_kv_batch* b, const int32_t* table, const np_kv_rows* r,
+                               const np_qk_norm* norm, const np_rotary* rot, void* pool, void* ws,
+                               hipStream_t stream) {
+  np_status st = check_kv_shape(s);
+  if (st == NP_OK) st = check_batch(fn, s, layer, b);
+  if (st != NP_OK) return st;
+  if (!r) return fail(NP_ERR_INVALID_ARG, "%s: rows is NULL", fn);
+  const int n = b->n_tokens;
+  if ((st = check_rows(fn, "q", s, r->q, r->q_stride, s->heads, n)) != NP_OK ||
+      (st = check_rows(fn, "k", s, r->k, r->k_stride, s->kv_heads, n)) != NP_OK ||
+      (st = check_rows(fn, "v", s, r->v, r->v_stride, s->kv_heads, n)) != NP_OK ||
+      (st = check_rows(fn, "q_out", s, r->q_out, r->q_out_stride, s->heads, n)) != NP_OK)
+    return st;
+  if (r->q_out == r->q && n > 0 && r->q_out_stride != r->q_stride)
+    return fail(NP_ERR_INVALID_ARG, "%s: in place, but q_out_stride differs from q_stride", fn);
+  if (norm) {
+    if (!std::isfinite(norm->eps) || norm->eps < 0)
+      return fail(NP_ERR_INVALID_ARG, "%s: eps %g is not a finite number >= 0", fn,
+                  (double)norm->eps);
+    if (!aligned16_or_null(norm->q_weight) || !aligned16_or_null(norm->k_weight))
+      return fail(NP_ERR_INVALID_ARG, "%s: weights must be 16-byte aligned", fn);
+  }
+  if (rot) {
+    if (rot->dim < 16 || rot->dim % 16 || rot->dim > s->head_dim)
+      return fail(NP_ERR_INVALID_ARG, "%s: rotary dim %d is not a multiple of 16 in [16, %d]", fn,
+                  rot->dim, s->head_dim);
+    if (rot->max_pos < 1) return fail(NP_ERR_INVALID_ARG, "%s: max_pos %d < 1", fn, rot->max_pos);
+    if (!aligned16(rot->cos) || !aligned16(rot->sin))
+      return fail(NP_ERR_INVALID_ARG, "%s: cos and sin must be non-NULL and 16-byte aligned", fn);
+  }
+  if (!aligned16(table) || !aligned16(pool) || !aligned16(ws))
+    return fail(NP_ERR_INVALID_ARG, "%s: pointers must be non-NULL and 16-byte aligned", fn);
+  if (b->n_seq == 0 || b->n_tokens == 0) return NP_OK;
+  hipError_t e = launch_kv_append(*s, layer, *b, table, *r, norm, rot, pool, ws, stream);
+  return e == hipSuccess ? NP_OK : hip_fail(e, fn);
+}
+
 static np_status attn_common(const char* fn, const np_kv_shape* s, int32_t layer,
-                             const np_kv_batch* b, const int32_t* table, const void* q,
-                             int64_t q_stride, const void* pool, float scale, int32_t window,
-                             void* out, int64_t out_stride, void* ws, hipStream_t stream) {
+                             const np_kv_batch* b, const np_kv_shared* shared,
+                             const int32_t* table, const void* q, int64_t q_stride,
+                             const void* pool, float scale, int32_t window, void* out,
+                             int64_t out_stride, void* ws, hipStream_t stream) {
   np_status st = check_kv_shape(s);
   if (st == NP_OK) st = check_batch(fn, s, layer, b);
   if (st == NP_OK) st = check_rows(fn, "q", s, q, q_stride, s->heads, b->n_tokens);
@@ -91,8 +135,11 @@ static np_status attn_common(const char* fn, const np_kv_shape* s, int32_t layer
   if (out == q && b->n_tokens > 0 && out_stride != q_stride)
     return fail(NP_ERR_INVALID_ARG, "%s: in place, but out_stride differs from q_stride", fn);
   if (b->n_seq == 0 || b->n_tokens == 0) return NP_OK;
-  hipError_t e = launch_attn(*s, layer, *b, table, q, q_stride, pool, scale, window, out,
-                             out_stride, ws, stream);
+  hipError_t e =
+      shared ? launch_attn_shared(*s, layer, *b, *shared, table, q, q_stride, pool, scale, window,
+                                  out, out_stride, ws, stream)
+             : launch_attn(*s, layer, *b, table, q, q_stride, pool, scale, window, out, out_stride,
+                           ws, stream);
   return e == hipSuccess ? NP_OK : hip_fail(e, fn);
 }
 
@@ -182,32 +229,31 @@ np_status np_kv_compact(const np_kv_shape* s, const np_kv_state* state, void* po
 np_status np_kv_append(const np_kv_shape* s, int32_t layer, const np_kv_batch* b,
                        const int32_t* table, const np_kv_rows* r, const np_rotary* rot, void* pool,
                        void* ws, hipStream_t stream) {
-  const char* fn = "np_kv_append";
+  return append_common("np_kv_append", s, layer, b, table, r, nullptr, rot, pool, ws, stream);
+}
+
+np_status np_kv_append_norm(const np_kv_shape* s, int32_t layer, const np_kv_batch* b,
+                            const int32_t* table, const np_kv_rows* r, const np_qk_norm* norm,
+                            const np_rotary* rot, void* pool, void* ws, hipStream_t stream) {
+  return append_common("np_kv_append_norm", s, layer, b, table, r, norm, rot, pool, ws, stream);
+}
+
+np_status np_kv_read(const np_kv_shape* s, int32_t layer, const np_kv_batch* b,
+                     const int32_t* table, const void* pool, void* k, int64_t k_stride, void* v,
+                     int64_t v_stride, void* ws, hipStream_t stream) {
+  const char* fn = "np_kv_read";
   np_status st = check_kv_shape(s);
   if (st == NP_OK) st = check_batch(fn, s, layer, b);
+  if (st == NP_OK && k) st = check_rows(fn, "k_out", s, k, k_stride, s->kv_heads, b->n_tokens);
+  if (st == NP_OK && v) st = check_rows(fn, "v_out", s, v, v_stride, s->kv_heads, b->n_tokens);
   if (st != NP_OK) return st;
-  if (!r) return fail(NP_ERR_INVALID_ARG, "%s: rows is NULL", fn);
-  const int n = b->n_tokens;
-  if ((st = check_rows(fn, "q", s, r->q, r->q_stride, s->heads, n)) != NP_OK ||
-      (st = check_rows(fn, "k", s, r->k, r->k_stride, s->kv_heads, n)) != NP_OK ||
-      (st = check_rows(fn, "v", s, r->v, r->v_stride, s->kv_heads, n)) != NP_OK ||
-      (st = check_rows(fn, "q_out", s, r->q_out, r->q_out_stride, s->heads, n)) != NP_OK)
-    return st;
-  if (r->q_out == r->q && n > 0 && r->q_out_stride != r->q_stride)
-    return fail(NP_ERR_INVALID_ARG, "%s: in place, but q_out_stride differs from q_stride", fn);
-  if (rot) {
-    if (rot->dim < 16 || rot->dim % 16 || rot->dim > s->head_dim)
-      return fail(NP_ERR_INVALID_ARG, "%s: rotary dim %d is not a multiple of 16 in [16, %d]", fn,
-                  rot->dim, s->head_dim);
-    if (rot->max_pos < 1) return fail(NP_ERR_INVALID_ARG, "%s: max_pos %d < 1", fn, rot->max_pos);
-    if (!aligned16(rot->cos) || !aligned16(rot->sin))
-      return fail(NP_ERR_INVALID_ARG, "%s: cos and sin must be non-NULL and 16-byte aligned", fn);
-  }
   if (!aligned16(table) || !aligned16(pool) || !aligned16(ws))
     return fail(NP_ERR_INVALID_ARG, "%s: pointers must be non-NULL and 16-byte aligned", fn);
-  if (b->n_seq == 0 || b->n_tokens == 0) return NP_OK;
-  hipError_t e = launch_kv_append(*s, layer, *b, table, *r, rot, pool, ws, stream);
-  return e == hipSuccess ? NP_OK : hip_fail(e, "np_kv_append launch");
+  if (k && k == v && b->n_tokens > 0)
+    return fail(NP_ERR_INVALID_ARG, "%s: k_out and v_out are the same", fn);
+  if (b->n_seq == 0 || b->n_tokens == 0 || (!k && !v)) return NP_OK;
+  hipError_t e = launch_kv_read(*s, layer, *b, table, pool, k, k_stride, v, v_stride, ws, stream);
+  return e == hipSuccess ? NP_OK : hip_fail(e, fn);
 }
 
 np_status np_attn_decode(const np_kv_shape* s, int32_t layer, const np_kv_batch* b,
@@ -217,15 +263,31 @@ np_status np_attn_decode(const np_kv_shape* s, int32_t layer, const np_kv_batch*
   if (b && b->cu_tokens)
     return fail(NP_ERR_INVALID_ARG,
                 "np_attn_decode: one token per row, cu_tokens must be NULL (np_attn_prompt)");
-  return attn_common("np_attn_decode", s, layer, b, table, q, q_stride, pool, scale, window, out,
-                     out_stride, ws, stream);
+  return attn_common("np_attn_decode", s, layer, b, nullptr, table, q, q_stride, pool, scale, window,
+                     out, out_stride, ws, stream);
 }
 
 np_status np_attn_prompt(const np_kv_shape* s, int32_t layer, const np_kv_batch* b,
                          const int32_t* table, const void* q, int64_t q_stride, const void* pool,
                          float scale, int32_t window, void* out, int64_t out_stride, void* ws,
                          hipStream_t stream) {
-  return attn_common("np_attn_prompt", s, layer, b, table, q, q_stride, pool, scale, window, out,
+  return attn_common("np_attn_prompt", s, layer, b, nullptr, table, q, q_stride, pool, scale, window,
+                     out, out_stride, ws, stream);
+}
+
+np_status np_attn_decode_shared(const np_kv_shape* s, int32_t layer, const np_kv_batch* b,
+                                const np_kv_shared* shared, const int32_t* table, const void* q,
+                                int64_t q_stride, const void* pool, float scale, int32_t window,
+                                void* out, int64_t out_stride, void* ws, hipStream_t stream) {
+  const char* fn = "np_attn_decode_shared";
+  if (b && b->cu_tokens)
+    return fail(NP_ERR_INVALID_ARG, "%s: one token per row, cu_tokens must be NULL", fn);
+  if (!shared) return fail(NP_ERR_INVALID_ARG, "%s: shared is NULL", fn);
+  if (shared->max_prefix < 0)
+    return fail(NP_ERR_INVALID_ARG, "%s: max_prefix %d < 0", fn, shared->max_prefix);
+  if (b && b->n_seq > 0 && (!aligned4(shared->lead) || !aligned4(shared->prefix)))
+    return fail(NP_ERR_INVALID_ARG, "%s: lead and prefix must be non-NULL and 4-byte aligned", fn);
+  return attn_common(fn, s, layer, b, shared, table, q, q_stride, pool, scale, window, out,
                      out_stride, ws, stream);
 }
 

@@ -287,15 +287,16 @@ struct RowsCfg {
 // sequence with page table trow.  minpos and maxpos bound the rows' positions.
 // Each wave takes every fourth step, and has its own maximum m, sum l and
 // outputs o afterwards; missing: a key had no page.
-template <class T, int DP, bool FULL, bool E8, class C = RowsCfg<T, DP, E8>>
-__device__ __forceinline__ void rows_keys(const AttnArgs& a, const int32_t* trow, int h, int minpos,
-                                          int maxpos, int kbeg, int kend, int k0, int k1,
+// CUT: the rows may see keys before kbeg or from kend on, which other stretches have.
+template <class T, int DP, bool FULL, bool E8, bool CUT, class C = RowsCfg<T, DP, E8>>
+__device__ __forceinline__ void rows_keys(int tid, const AttnArgs& a, const int32_t* trow, int h,
+                                          int minpos, int maxpos, int kbeg, int kend, int k0, int k1,
                                           const char* qp, int qpos, f32x4 (&o)[C::VS][C::NV],
                                           float& m, float& l, bool& missing) {
   constexpr int V = C::V, W = C::W, KS = C::KS, KT = C::KT, KD = C::KD, KP = C::KP, NS = C::NS,
                 NV = C::NV, VS = C::VS, VR = C::VR;
-  const int lane = threadIdx.x % WAVE;
-  const int wave = uniform((int)threadIdx.x / WAVE);
+  const int lane = tid % WAVE;
+  const int wave = uniform(tid / WAVE);
   const int r = lane & 15, g = lane >> 4;
   const int klast = max(kend - 1, 0);
   // page ids through the scalar cache.  A step of 32 keys has two pages when
@@ -429,7 +430,8 @@ __device__ __forceinline__ void rows_keys(const AttnArgs& a, const int32_t* trow
     load_v();
     __builtin_amdgcn_sched_barrier(0);
     const bool full = ok == 3 && base + KS - 1 <= minpos &&
-                      (a.window == 0 || base > maxpos - a.window);
+                      (a.window == 0 || base > maxpos - a.window) &&
+                      (!CUT || (base >= kbeg && base + KS <= kend));
     f32x4 sc[KT];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
@@ -461,7 +463,9 @@ __device__ __forceinline__ void rows_keys(const AttnArgs& a, const int32_t* trow
 #pragma unroll
       for (int i = 0; i < 4 * KT; ++i) {
         const int key = base + vk + i;
-        if (!has || key > qpos || (a.window && key <= qpos - a.window)) p[i] = -INFINITY;
+        if (!has || key > qpos || (a.window && key <= qpos - a.window) ||
+            (CUT && (key < kbeg || key >= kend)))
+          p[i] = -INFINITY;
       }
     }
     float mx = p[0];
@@ -552,6 +556,55 @@ __device__ __forceinline__ void rows_keys(const AttnArgs& a, const int32_t* trow
   }
 }
 
+// The four waves' results of rows_keys on their way through LDS: stored, and,
+// behind a barrier, four columns of a row joined (M, L: the row's maximum, sum).
+template <class C>
+__device__ __forceinline__ void rows_meet(const f32x4 (&o)[C::VS][C::NV], float m, float l,
+                                          float (&s_o)[NWAVE][RB][C::OP], float (&s_m)[NWAVE][RB],
+                                          float (&s_l)[NWAVE][RB]) {
+  constexpr int NV = C::NV;
+  const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
+  const int r = lane & 15, g = lane >> 4;
+  l = sum_groups(l);
+  if (g == 0) {
+    s_m[wave][r] = m;
+    s_l[wave][r] = l;
+  }
+#pragma unroll
+  for (int s = 0; s < C::VS; ++s)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < NV; j += 4)
+        *(float4*)&s_o[wave][r][16 * NV * s + NV * (4 * g + i) + j] =
+            make_float4(o[s][j][i], o[s][j + 1][i], o[s][j + 2][i], o[s][j + 3][i]);
+}
+
+template <class C>
+__device__ __forceinline__ float4 rows_met(const float (&s_o)[NWAVE][RB][C::OP],
+                                           const float (&s_m)[NWAVE][RB],
+                                           const float (&s_l)[NWAVE][RB], int qr, int d, float& M,
+                                           float& L) {
+  M = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < NWAVE; ++w) M = fmaxf(M, s_m[w][qr]);
+  float4 sum = make_float4(0, 0, 0, 0);
+  L = 0.f;
+#pragma unroll
+  for (int w = 0; w < NWAVE; ++w) {
+    const float mw = s_m[w][qr], lw = s_l[w][qr];
+    // without a maximum the sum is 0, or NaN when every score was
+    const float f = mw == -INFINITY ? lw : __builtin_amdgcn_exp2f(mw - M);
+    const float4 x = *(const float4*)&s_o[w][qr][d];
+    L += f * lw;
+    sum.x += f * x.x;
+    sum.y += f * x.y;
+    sum.z += f * x.z;
+    sum.w += f * x.w;
+  }
+  return sum;
+}
+
 // EVEN: one token a row, the keys of all rows dealt evenly to the workgroups;
 // otherwise a workgroup per (block, head, split).
 template <class T, int DP, bool FULL, bool EVEN, bool E8>
@@ -564,7 +617,7 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(
 
   const int lane = threadIdx.x % WAVE;
   const int wave = uniform((int)threadIdx.x / WAVE);
-  const int r = lane & 15, g = lane >> 4;
+  const int r = lane & 15;
 
   // One segment: block `blk` of head h of a batch row against keys [k0, k1) of
   // its [kal, kend).  With parts > 1 other workgroups have the block's other
@@ -582,26 +635,14 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(
   f32x4 o[VS][NV];
   float m, l;
   bool missing;
-  rows_keys<T, DP, FULL, E8>(
-      a, a.table + (int64_t)t.row.seq * a.M, h, t.minpos, t.maxpos, kbeg, kend, k0, k1,
+  rows_keys<T, DP, FULL, E8, false>(
+      threadIdx.x, a, a.table + (int64_t)t.row.seq * a.M, h, t.minpos, t.maxpos, kbeg, kend, k0, k1,
       a.q + (int64_t)(t.row.begin + tok) * a.q_stride + (int64_t)head * a.D * W, qpos, o, m, l,
       missing);
   if (missing && lane == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
 
   // the four waves' results meet in LDS
-  l = sum_groups(l);
-  if (g == 0) {
-    s_m[wave][r] = m;
-    s_l[wave][r] = l;
-  }
-#pragma unroll
-  for (int s = 0; s < VS; ++s)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < NV; j += 4)
-        *(float4*)&s_o[wave][r][16 * NV * s + NV * (4 * g + i) + j] =
-            make_float4(o[s][j][i], o[s][j + 1][i], o[s][j + 2][i], o[s][j + 3][i]);
+  rows_meet<C>(o, m, l, s_o, s_m, s_l);
   __syncthreads();
   auto store_out = [&](int qr, int d, float4 sum, float L) {
     const float inv = 1.f / L;
@@ -620,23 +661,8 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(
   const __amdgpu_buffer_rsrc_t prs = make_rsrc(a.part, (uint32_t)KV_PART_ROWS * DP * 4);
   for (int u = threadIdx.x; u < t.nrow * TD; u += ROWS_T) {
     const int qr = u / TD, d = u % TD * 4;
-    float M = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < NWAVE; ++w) M = fmaxf(M, s_m[w][qr]);
-    float4 sum = make_float4(0, 0, 0, 0);
-    float L = 0.f;
-#pragma unroll
-    for (int w = 0; w < NWAVE; ++w) {
-      const float mw = s_m[w][qr], lw = s_l[w][qr];
-      // without a maximum the sum is 0, or NaN when every score was
-      const float f = mw == -INFINITY ? lw : __builtin_amdgcn_exp2f(mw - M);
-      const float4 x = *(const float4*)&s_o[w][qr][d];
-      L += f * lw;
-      sum.x += f * x.x;
-      sum.y += f * x.y;
-      sum.z += f * x.z;
-      sum.w += f * x.w;
-    }
+    float M, L;
+    const float4 sum = rows_met<C>(s_o, s_m, s_l, qr, d, M, L);
     if (parts > 1) {
       const uint32_t row = slot * a.prow + qr;
       buf_store16_agent(prs, (row * DP + d) * 4, sum);
@@ -919,13 +945,14 @@ struct TileCfg {
 // h, against a tile's rows: this lane's query at qp has position qpos, those of its
 // wave lie in [wmin, wmax].  Afterwards a lane has its query's maximum m, half of its sum l
 // (the other half is lane ^ 32's) and its outputs o; missing: a key had no page.
-template <class T, int DP, bool FULL, bool E8, class C = TileCfg<DP, E8>>
-__device__ __forceinline__ void tile_keys(const AttnArgs& a, const int32_t* trow, int h, int kbeg,
-                                          int kend, int wmin, int wmax, const char* qp, int qpos,
+// CUT: the rows may see keys from kend on, which other stretches have.
+template <class T, int DP, bool FULL, bool E8, bool CUT, class C = TileCfg<DP, E8>>
+__device__ __forceinline__ void tile_keys(int tid, const AttnArgs& a, const int32_t* trow, int h,
+                                          int kbeg, int kend, int wmin, int wmax, const char* qp, int qpos,
                                           char* s_k, char* s_v, f32x16 (&o)[C::DT], float& m,
                                           float& l, bool& missing) {
   constexpr int KB = C::KB, NL = C::NL, RSTEP = C::RSTEP, KT = C::KT, KD = DP / 16, DT = C::DT;
-  const int tid = threadIdx.x, lane = tid % WAVE;
+  const int lane = tid % WAVE;
   const int wave = uniform(tid / WAVE);
   const int r = lane & 31, h2 = lane >> 5;
   // a negative scale turns into negated queries, so that the largest q.k has
@@ -1097,7 +1124,8 @@ __device__ __forceinline__ void tile_keys(const AttnArgs& a, const int32_t* trow
       load_pages(base + 2 * KB);
     }
     if (base <= wmax && (a.window == 0 || base + KB - 1 > wmin - a.window)) {
-      const bool full = !bad && base + KB - 1 <= wmin && (a.window == 0 || base > wmax - a.window);
+      const bool full = !bad && base + KB - 1 <= wmin &&
+                        (a.window == 0 || base > wmax - a.window) && (!CUT || base + KB <= kend);
       const uint32_t bo = buf * KB * C::ROW;
       f32x16 sc[KT];
 #pragma unroll
@@ -1115,7 +1143,8 @@ __device__ __forceinline__ void tile_keys(const AttnArgs& a, const int32_t* trow
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int key = base + 32 * kt + 8 * (i / 4) + 4 * h2 + i % 4;
-            if (key > qpos || (a.window && key <= qpos - a.window)) sc[kt][i] = -INFINITY;
+            if (key > qpos || (a.window && key <= qpos - a.window) || (CUT && key >= kend))
+              sc[kt][i] = -INFINITY;
           }
         if (bad) {
           uint32_t hide = 0;  // bit 16 kt + i
@@ -1225,7 +1254,7 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
   f32x16 o[DT];
   float m, l;
   bool missing;
-  tile_keys<T, DP, FULL, E8>(a, a.table + (size_t)t.row.seq * a.M, h, kbeg, kend, wmin, wmax, qp,
+  tile_keys<T, DP, FULL, E8, false>(tid, a, a.table + (size_t)t.row.seq * a.M, h, kbeg, kend, wmin, wmax, qp,
                              qpos, s_k, s_v, o, m, l, missing);
   if (missing && lane == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
 

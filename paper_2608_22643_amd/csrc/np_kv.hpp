@@ -22,6 +22,8 @@ namespace np {
 //   partials       of split attention rows: fp32 [KV_PART_ROWS][DP] outputs,
 //                  then fp32 [KV_PART_ROWS][2] (maximum, sum); as many rows as
 //                  two tiles of 128 on every compute unit, split in two
+//   shared plan    of np_attn_decode_shared: int32 [KV_SHARED_HEADS] twice (the
+//                  workgroups of a part), [S] (a row's lead)
 // Zeros and counts have to last from call to call, so they come before
 // everything whose size depends on the shape: one workspace serves caches of
 // several shapes in turn.
@@ -31,6 +33,7 @@ constexpr int KV_PART_ROWS = 131072;
 constexpr size_t KV_ZEROS = 8192;
 constexpr int KV_MAX_BLOCKS = 8192;
 constexpr int KV_MAX_SEQS = 4096;
+constexpr int KV_SHARED_HEADS = 32768;  // most query heads of a batch that np_attn_decode_shared splits
 
 inline int kv_dpad(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
@@ -39,6 +42,7 @@ struct KvScratch {
   char* zeros;
   int32_t* count;
   float *part, *ml;
+  int32_t *shared_p, *shared_s, *shared_lead;
 };
 inline size_t kv_ws_layout(const np_kv_shape& s, char* ws, KvScratch* k) {
   size_t at = WS_CTRL_BYTES;
@@ -55,6 +59,9 @@ inline size_t kv_ws_layout(const np_kv_shape& s, char* ws, KvScratch* k) {
   for (int32_t** p : {&t.off, &t.split}) *p = (int32_t*)take((size_t)(s.max_seqs + 1) * 4);
   t.part = (float*)take((size_t)KV_PART_ROWS * kv_dpad(s.head_dim) * 4);
   t.ml = (float*)take((size_t)KV_PART_ROWS * 2 * 4);
+  t.shared_p = (int32_t*)take(KV_SHARED_HEADS * 4);
+  t.shared_s = (int32_t*)take(KV_SHARED_HEADS * 4);
+  t.shared_lead = (int32_t*)take((size_t)s.max_seqs * 4);
   if (k) *k = t;
   return at;
 }

@@ -293,10 +293,11 @@ np_status np_attn_prompt(const np_kv_shape* shape, int32_t layer, const np_kv_ba
 /* np_attn_decode for rows that share prefixes: the same outputs (up to the
  * rounding of sums in another order; the same bits from run to run), but the
  * keys and values of a group's prefix are read once for its rows together, each
- * row's other keys after that.  Two kernels, the second to join the parts; where
- * nothing can be gained (max_prefix 0; a batch of more than 32768 query heads in
- * all; more than 128 query heads per key-value head, 16 in fp32) it is
- * np_attn_decode, leads and prefixes then unread. */
+ * row's other keys after that.  Two kernels, the second to join the parts.  Where
+ * little can be gained (max_prefix and the batch bound what sharing saves: up to
+ * some 30 MB of keys and values it is not worth the second kernel), and for batches
+ * of more than 32768 query heads in all, or more than 128 query heads per key-value
+ * head (16 in fp32), it is np_attn_decode, leads and prefixes then unread. */
 np_status np_attn_decode_shared(const np_kv_shape* shape, int32_t layer, const np_kv_batch* batch,
                                 const np_kv_shared* shared, const int32_t* page_table,
                                 const void* q, int64_t q_stride, const void* pool, float scale,

@@ -299,6 +299,9 @@ __device__ __forceinline__ void rows_keys(int tid, const AttnArgs& a, const int3
   const int wave = uniform(tid / WAVE);
   const int r = lane & 15, g = lane >> 4;
   const int klast = max(kend - 1, 0);
+  // the keys that this lane's query counts
+  const int klast_seen = CUT ? min(qpos, kend - 1) : qpos;
+  const int kfirst_seen = max(a.window ? qpos - a.window + 1 : 0, CUT ? kbeg : 0);
   // page ids through the scalar cache.  A step of 32 keys has two pages when
   // P is 16.
   struct Pages {
@@ -463,9 +466,7 @@ __device__ __forceinline__ void rows_keys(int tid, const AttnArgs& a, const int3
 #pragma unroll
       for (int i = 0; i < 4 * KT; ++i) {
         const int key = base + vk + i;
-        if (!has || key > qpos || (a.window && key <= qpos - a.window) ||
-            (CUT && (key < kbeg || key >= kend)))
-          p[i] = -INFINITY;
+        if (!has || key > klast_seen || key < kfirst_seen) p[i] = -INFINITY;
       }
     }
     float mx = p[0];
@@ -501,10 +502,10 @@ __device__ __forceinline__ void rows_keys(int tid, const AttnArgs& a, const int3
                       __float_as_uint(p[3]));
     }
     __builtin_amdgcn_sched_barrier(0);
+    float f[VR];
     if constexpr (E8) {
       // the rows' scales; of a row that repeats another one, and has no weight,
       // any that is finite
-      float f[VR];
       const bool inside = base >= kbeg && base + KS <= kend;
 #pragma unroll
       for (int e = 0; e < VR; ++e) {
@@ -512,30 +513,36 @@ __device__ __forceinline__ void rows_keys(int tid, const AttnArgs& a, const int3
         if (!inside) b = base + vk + e < kbeg || base + vk + e > klast ? 127u : b;
         f[e] = scale_of_byte(b);
       }
-#pragma unroll
-      for (int s = 0; s < VS; ++s)
-#pragma unroll
-        for (int e = 0; e < VR; ++e) {
-          const u32x4_t x = vf[e][s];
-          vf[e][s] = elements16<T>(x, 0, f[e]);
-        }
     }
 #pragma unroll
-    for (int s = 0; s < VS; ++s)
+    for (int s = 0; s < VS; ++s) {
+      uint32_t w[VR];  // 16-bit types: elements j & ~1 and j | 1 of each row
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         uint4 av;
         if constexpr (V == 8) {
+          if (j % 2 == 0)
+#pragma unroll
+            for (int e = 0; e < VR; ++e) {
+              if constexpr (E8) w[e] = element_pair<T>(vf[e][s][j / 4], f[e], j % 4 == 2);
+              else w[e] = vf[e][s][j / 2];
+            }
           const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;  // high or low halves
-          av.x = __builtin_amdgcn_perm(vf[1][s][j / 2], vf[0][s][j / 2], sel);
-          av.y = __builtin_amdgcn_perm(vf[3][s][j / 2], vf[2][s][j / 2], sel);
-          av.z = __builtin_amdgcn_perm(vf[5][s][j / 2], vf[4][s][j / 2], sel);
-          av.w = __builtin_amdgcn_perm(vf[7][s][j / 2], vf[6][s][j / 2], sel);
+          av.x = __builtin_amdgcn_perm(w[1], w[0], sel);
+          av.y = __builtin_amdgcn_perm(w[3], w[2], sel);
+          av.z = __builtin_amdgcn_perm(w[5], w[4], sel);
+          av.w = __builtin_amdgcn_perm(w[7], w[6], sel);
+        } else if constexpr (E8) {
+#pragma unroll
+          for (int e = 0; e < VR; ++e)
+            w[e] = __float_as_uint(element_pair_f32(vf[e][s].x, f[e], j >= 2)[j & 1]);
+          av = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
           av = make_uint4(vf[0][s][j], vf[1][s][j], vf[2][s][j], vf[3][s][j]);
         }
         o[s][j] = mfma_step<T>(av, pb, o[s][j]);
       }
+    }
     if constexpr (!LAST) {
       ok = next_ok;
       missing |= ok != 3;
@@ -608,7 +615,7 @@ __device__ __forceinline__ float4 rows_met(const float (&s_o)[NWAVE][RB][C::OP],
 // EVEN: one token a row, the keys of all rows dealt evenly to the workgroups;
 // otherwise a workgroup per (block, head, split).
 template <class T, int DP, bool FULL, bool EVEN, bool E8>
-__global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_rows_kernel(
+__global__ __launch_bounds__(ROWS_T, DP < 256 ? (E8 ? 3 : 2) : E8 ? 2 : 1) void attn_rows_kernel(
     AttnArgs a) {
   using C = RowsCfg<T, DP, E8>;
   constexpr int V = C::V, W = C::W, KS = C::KS, NV = C::NV, VS = C::VS;
@@ -1097,6 +1104,10 @@ __device__ __forceinline__ void tile_keys(int tid, const AttnArgs& a, const int3
       }
   }
 
+  // the keys that this lane's query counts
+  const int klast_seen = CUT ? min(qpos, kend - 1) : qpos;
+  const int kfirst_seen = a.window ? qpos - a.window + 1 : 0;
+
   // LDS addresses of a lane.  K: piece 2 s + h2 of row r (+ 32 kt); V: four
   // columns of rows vr and vr + 8 (+ 16 mm), column 32 j + vc.  The pieces' xor
   // with s or j can be taken on the whole address, since rows are aligned.
@@ -1115,6 +1126,17 @@ __device__ __forceinline__ void tile_keys(int tid, const AttnArgs& a, const int3
   }
   __syncthreads();
   int buf = 0;
+  if (CUT && wmax < 0) {  // a wave without rows: its share of the loads
+    for (int base = k0; base < kend; base += KB, buf ^= 1) {
+      if (base + KB < kend) {
+        load_rows(base + KB);
+        load_pages(base + 2 * KB);
+        store_rows(buf ^ 1);
+      }
+      __syncthreads();
+    }
+    return;
+  }
   for (int base = k0; base < kend; base += KB, buf ^= 1) {
     const bool more = base + KB < kend;
     bad = next_bad;
@@ -1123,7 +1145,9 @@ __device__ __forceinline__ void tile_keys(int tid, const AttnArgs& a, const int3
       load_rows(base + KB);
       load_pages(base + 2 * KB);
     }
-    if (base <= wmax && (a.window == 0 || base + KB - 1 > wmin - a.window)) {
+    // CUT: all steps count; a step left out would cost moves of the outputs
+    // between registers in every other one
+    if (CUT || (base <= wmax && (a.window == 0 || base + KB - 1 > wmin - a.window))) {
       const bool full = !bad && base + KB - 1 <= wmin &&
                         (a.window == 0 || base > wmax - a.window) && (!CUT || base + KB <= kend);
       const uint32_t bo = buf * KB * C::ROW;
@@ -1143,8 +1167,7 @@ __device__ __forceinline__ void tile_keys(int tid, const AttnArgs& a, const int3
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int key = base + 32 * kt + 8 * (i / 4) + 4 * h2 + i % 4;
-            if (key > qpos || (a.window && key <= qpos - a.window) || (CUT && key >= kend))
-              sc[kt][i] = -INFINITY;
+            if (key > klast_seen || key < kfirst_seen) sc[kt][i] = -INFINITY;
           }
         if (bad) {
           uint32_t hide = 0;  // bit 16 kt + i
@@ -1403,7 +1426,7 @@ hipError_t launch_rows(AttnArgs a, int64_t keys, int max_tokens, hipStream_t str
   dim3 grid;
   if (even) {
     a.chunk = (int)((groups + MAX_SPLITS - 3) / (MAX_SPLITS - 2));
-    grid.x = 512;
+    grid.x = E8 && DP <= 128 ? 768 : 512;
   } else {
     const int64_t least = ones ? GROUP : 256;
     int64_t splits = small                  ? groups

@@ -6,7 +6,8 @@
 //     out = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i,   M = max_i m_i.
 // So a group's prefix is one part of all its rows, and the query heads of those
 // rows are rows of one tile against it: a key or value is read once for up to
-// 128 of them.  Each row's own keys are row blocks as in np_attn_decode.
+// 128 of them.  Small groups, all of fp32, and each row's own keys are row blocks
+// as in np_attn_decode: 16 query heads against keys in registers.
 //
 // One kernel computes the parts, a second joins them.  The parts' keys lie on
 // a line (the tiles' first), weighed by what they cost, and every workgroup
@@ -21,29 +22,35 @@ namespace np {
 
 namespace {
 
+// A block on the line: `units` (steps of a tile, or groups of a row's own keys)
+// of weight W behind a stretch of weight FIX for its beginning and end.  Unit u
+// lies at FIX + u W of its block, and belongs to the workgroup whose stretch has
+// that place.
+struct Cost {
+  int fix, w;
+  __device__ int block(int units) const { return fix + units * w; }
+  // the first unit at or past place x of a block
+  __device__ int unit(int x) const { return x > fix ? (x - fix + w - 1) / w : 0; }
+  __device__ int place(int unit) const { return fix + unit * w; }
+};
+
 struct SharedArgs {
   AttnArgs a;
   const int32_t *lead, *prefix;
   int max_prefix;
   int Hq, n;
   int least;  // weight of a stretch at least
+  int small;  // most query heads per key-value head of a group that has row blocks
+  Cost tile, own;
   int32_t *info_p, *info_s, *row_lead;
+  __device__ Cost cost(bool is_tile) const {
+    return {is_tile ? tile.fix : own.fix, is_tile ? tile.w : own.w};
+  }
 };
 
-constexpr int SH_WG = 512;     // workgroups at most
-constexpr int FAR = 1 << 30;    // past all positions
-constexpr int OWN_WEIGHT = 4;  // of 128 keys of a row: the line counts 32 keys
+constexpr int SH_WG = 512;    // workgroups at most
+constexpr int FAR = 1 << 30;  // past all positions
 static_assert(2 * KV_SHARED_HEADS + SH_WG * TB <= KV_PART_ROWS, "rows of all parts fit");
-
-// What a block of shared keys is for type T: 128 rows against steps through LDS,
-// or 16 rows against 128 keys in registers (fp32).
-template <class T, int DP, bool E8>
-struct SharedCfg {
-  static constexpr bool TILE = T::V == 8;
-  static constexpr int ROWS = TILE ? TB : RB;
-  static constexpr int KEYS = TILE ? TileCfg<DP, E8>::KB : GROUP;
-  static constexpr int WEIGHT = KEYS / 32;
-};
 
 __device__ inline int div_up_pos(int a, int b) { return a > 0 ? (a + b - 1) / b : 0; }
 
@@ -59,12 +66,15 @@ struct SharedRow {
   int prefix;  // positions it has in common with it
   int seq;     // the lead's sequence
   int run;     // the first of the neighbouring rows that name the same lead
+  int name;    // the lead that the row names
+  bool tile;   // the group's blocks are tiles
 };
 __device__ inline SharedRow shared_row(const SharedArgs& x, int i0, int run_before, int32_t* err) {
   const int lane = threadIdx.x % WAVE, n = x.n;
   const int i = min(i0 + lane, n - 1);
   SharedRow s;
   const int L = x.lead[i], before = x.lead[max(i - 1, 0)], after = x.lead[min(i + 1, n - 1)];
+  s.name = L;
   s.row = lane_row(x.a.b, i, err);
   const uint64_t cuts = __ballot(i == 0 || before != L) & (~0ull >> (WAVE - 1 - lane));
   s.run = cuts ? i0 + 63 - __clzll((long long)cuts) : run_before;
@@ -72,6 +82,9 @@ __device__ inline SharedRow shared_row(const SharedArgs& x, int i0, int run_befo
   const int at = ok ? L : 0;
   s.prefix = x.prefix[at];
   s.seq = x.a.b.seqs ? x.a.b.seqs[at] : at;
+  // whether the group has more rows than `small` (the same answer for all of them)
+  const int past = at + x.small / x.a.G;
+  s.tile = past < n && x.lead[past] == at;
   ok = ok && s.prefix >= 0 && s.prefix <= x.max_prefix && s.seq >= 0 && s.seq < x.a.b.S;
   if (!ok && err && i0 + lane < n) atomicOr(err, NP_DEVERR_STATE);
   const bool alone = L == i && (i + 1 >= n || after != L);
@@ -102,9 +115,12 @@ __device__ inline int own_tid() {
 
 __device__ inline int lane_max(int v) { return (int)wave_max((uint32_t)(v + 1)) - 1; }  // v >= -1
 
+// Rows of the batch in a block of shared keys.
+__device__ inline int block_rows(bool tile, int G) { return (tile ? TB : RB) / G; }
+
 template <class T, int DP, bool FULL, bool E8>
 __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(SharedArgs x) {
-  using P = SharedCfg<T, DP, E8>;
+  constexpr bool TILES = T::V == 8;
   using C = RowsCfg<T, DP, E8>;
   using TC = TileCfg<DP, E8>;
   constexpr int W = C::W, KS = C::KS;
@@ -112,36 +128,38 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
     float o[NWAVE][RB][C::OP];
     float m[NWAVE][RB], l[NWAVE][RB];
   };
-  constexpr int TILE_LDS = P::TILE ? 4 * TC::KB * TC::ROW : 0;
+  constexpr int TILE_LDS = TILES ? 4 * TC::KB * TC::ROW : 0;
   constexpr int LDS = TILE_LDS > (int)sizeof(RowsLds) ? TILE_LDS : (int)sizeof(RowsLds);
   __shared__ __attribute__((aligned(1024))) char lds[LDS];
   // of the rows i0 .. i0 + 63 (each wave finds the same): what would stand in the
   // way of the tiles' registers
   __shared__ struct {
-    int steps[WAVE], up_at[WAVE], lead[WAVE], prefix[WAVE], lead_seq[WAVE];
-    int us[WAVE], us_at[WAVE], p0[WAVE], seq[WAVE];
+    int steps[WAVE], up_at[WAVE], lead[WAVE], name[WAVE], prefix[WAVE], lead_seq[WAVE], tile[WAVE];
+    int groups[WAVE], us_at[WAVE], p0[WAVE], seq[WAVE];
   } rows;
   RowsLds& rl = *(RowsLds*)lds;
 
   const AttnArgs& a = x.a;
   const int lane = threadIdx.x % WAVE;
   const int wave = uniform((int)threadIdx.x / WAVE);
-  const int n = x.n, RT = P::ROWS / a.G;       // rows of the batch in a tile
+  const int n = x.n;
   const int per = (a.G + RB - 1) / RB, nb = per * a.Hkv;
   int32_t* const err = blockIdx.x == 0 && threadIdx.x < WAVE ? a.err : nullptr;
 
-  // A lane's row, its units on the line (up: steps of its tile, all heads; us:
-  // groups of its own keys), and theirs up to it.
+  // A lane's row, its blocks' weight on the line (up: its tile of all heads, us:
+  // its own keys), and the weights up to it.
   SharedRow sr;
-  int steps, up, us, up_at, us_at;
+  int steps, groups, up, us, up_at, us_at;
   auto load = [&](int first, int run_before, int32_t* e) {
     sr = shared_row(x, first, run_before, e);
     const bool here = first + lane < n;
-    steps = sr.lead >= 0 && here && (first + lane - sr.lead) % RT == 0
-                ? div_up_pos(sr.prefix, P::KEYS)
+    if (!TILES) sr.tile = false;
+    steps = sr.lead >= 0 && here && (first + lane - sr.lead) % block_rows(sr.tile, a.G) == 0
+                ? div_up_pos(sr.prefix, sr.tile ? TC::KB : GROUP)
                 : 0;
-    up = steps * a.Hkv;
-    us = here ? own_groups<KS>(sr.row.p0, sr.prefix, a.window) * nb : 0;
+    groups = own_groups<KS>(sr.row.p0, sr.prefix, a.window);
+    up = steps ? x.cost(sr.tile).block(steps) * a.Hkv : 0;
+    us = here ? x.own.block(groups) * nb : 0;
     up_at = (int)wave_incl_scan((uint32_t)up);
     us_at = (int)wave_incl_scan((uint32_t)us);
   };
@@ -152,130 +170,135 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
     run = last(sr.run);
     tp += last(up_at);
     ts += last(us_at);
-    if (err && i + lane < n) x.row_lead[i + lane] = sr.lead;
+    if (err && i + lane < n) x.row_lead[i + lane] = sr.lead < 0 ? -1 : sr.lead * 2 + sr.tile;
   }
   tp = uniform(tp);
-  ts = uniform(ts);
-  const int total = tp * P::WEIGHT + ts * OWN_WEIGHT;
+  const int total = tp + uniform(ts);
   const int share = max(x.least, (total + (int)gridDim.x - 1) / (int)gridDim.x);
   // workgroups go round the eight XCDs; each XCD gets one stretch in a piece
   const int wg = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
   if ((int64_t)wg * share >= total) return;
   const int beg = wg * share, end = min(total, beg + share);
-  const int s0 = min(tp, div_up_pos(beg, P::WEIGHT)), s1 = min(tp, div_up_pos(end, P::WEIGHT));
-  const int g0 = div_up_pos(beg - tp * P::WEIGHT, OWN_WEIGHT);
-  const int g1 = min(ts, div_up_pos(end - tp * P::WEIGHT, OWN_WEIGHT));
 
   // where the row of query head hq of batch row b goes, for the first part of
   // its block and for a further one
   auto part_of = [&](bool first, int base, int b, int hq, int local) {
-    return first ? base + b * x.Hq + hq : 2 * n * x.Hq + wg * P::ROWS + local;
+    return first ? base + b * x.Hq + hq : 2 * n * x.Hq + wg * TB + local;
   };
   auto put = [&](int row, int d, float4 v) { *(float4*)(a.part + (size_t)row * DP + d) = v; };
 
-  // steps [c0, c1) of a tile's: rows b0 .. of group L against its prefix
-  auto shared_part = [&](int b0, int L, int p, int seq, int h, int c0, int c1, bool first) {
-    const int tid = own_tid(), lane = tid % WAVE;
-    // its rows, and the positions they span
-    int cnt = 0;
-    for (int i = 0; i < RT && cnt == i; i += WAVE) {
-      const int b = b0 + i + lane;
-      const uint64_t out = ~__ballot(i + lane < RT && b < n && x.lead[min(b, n - 1)] == L);
-      cnt = i + (out ? __ffsll((unsigned long long)out) - 1 : WAVE);
-    }
-    int tmax = -1, tmin = FAR;
-    for (int i = 0; i < cnt; i += WAVE) {
-      const int p0 = i + lane < cnt ? lane_row(a.b, b0 + i + lane, nullptr).p0 : -1;
-      tmax = max(tmax, p0);
-      if (p0 >= 0) tmin = min(tmin, p0);
-    }
-    tmax = uniform(lane_max(tmax));
-    tmin = uniform(tmax < 0 ? 0 : FAR - lane_max(FAR - tmin));
-    cnt = uniform(cnt);
-    const int kbeg0 = a.window && tmax >= 0 ? max(0, tmin - a.window + 1) : 0;
-    const int kend0 = min(p, tmax + 1);
-    int kbeg = max(kbeg0, c0 * P::KEYS), kend = min(kend0, c1 * P::KEYS);
-    const int32_t* trow = a.table + (int64_t)seq * a.M;
-    // this lane's query
-    const int r = P::TILE ? wave * 32 + (lane & 31) : lane & 15;
-    const int rho = min(r, cnt * a.G - 1), b = b0 + rho / a.G, hq = h * a.G + rho % a.G;
-    const int p0 = lane_row(a.b, b, nullptr).p0;
-    const int qpos = p0 < 0 ? tmax : p0;  // of a row that is not served: nothing is made of it
-    const char* qp = a.q + (int64_t)b * a.q_stride + (int64_t)hq * a.D * W;
-    bool missing = false;
-    if constexpr (P::TILE) {
-      if (kbeg >= kend) kbeg = kend = 0;
-      f32x16 o[TC::DT];
-      float m, l;
-      // a wave without rows has nothing to compute, but its share of the loads
-      tile_keys<T, DP, FULL, E8, true>(tid, a, trow, h, kbeg, kend, tmin,
-                                       wave * 32 < cnt * a.G ? tmax : -1, qp, qpos, lds,
-                                       lds + TILE_LDS / 2, o, m, l, missing);
-      l = swap32_add(l, l);
-      if (r < cnt * a.G) {
-        const int h2 = lane >> 5;
-        const int row = part_of(first, 0, b, hq, r);
-#pragma unroll
-        for (int j = 0; j < TC::DT; ++j)
-#pragma unroll
-          for (int i = 0; i < 16; i += 4)
-            put(row, 32 * j + 2 * i + 4 * h2,
-                make_float4(o[j][i], o[j][i + 1], o[j][i + 2], o[j][i + 3]));
-        if (h2 == 0) *(float2*)(a.ml + (size_t)row * 2) = make_float2(m, l);
-      }
-    } else {
-      const int kal = kbeg / KS * KS;
-      if (kbeg >= kend) kbeg = kend = 0;
-      f32x4 o[C::VS][C::NV];
-      float m, l;
-      rows_keys<T, DP, FULL, E8, true>(tid, a, trow, h, tmin, tmax, kbeg, kend, kend ? kal : 0, kend, qp, qpos,
-                                 o, m, l, missing);
-      rows_meet<C>(o, m, l, rl.o, rl.m, rl.l);
-      __syncthreads();
-      for (int u = threadIdx.x; u < cnt * a.G * (DP / 4); u += ROWS_T) {
-        const int q = u / (DP / 4), d = u % (DP / 4) * 4;
-        float M, L2;
-        const float4 sum = rows_met<C>(rl.o, rl.m, rl.l, q, d, M, L2);
-        const int row = part_of(first, 0, b0 + q / a.G, h * a.G + q % a.G, q);
-        put(row, d, sum);
-        if (d == 0) *(float2*)(a.ml + (size_t)row * 2) = make_float2(M, L2);
-      }
-      __syncthreads();  // LDS is free again
-    }
-    if (missing && lane == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
+  int i0 = 0;
+  auto row_p0 = [&](int b) {
+    return b < i0 + WAVE ? rows.p0[b - i0] : lane_row(a.b, b, nullptr).p0;
   };
 
-  // groups [c0, c1) of block j of a row's own keys
-  auto own_part = [&](int b, int p0, int seq, int prefix, int j, int c0, int c1, bool first) {
+  // Units [c0, c1) of block j of row i0 + at: of its group's shared keys
+  // (shared), or of its own keys.
+  auto part = [&](bool shared, int at, int j, int c0, int c1) __attribute__((always_inline)) {
     const int tid = own_tid(), lane = tid % WAVE;
-    const int h = j % a.Hkv, q0 = j / a.Hkv * RB, rows = min(RB, a.G - q0);
-    const int kbeg = own_first<KS>(p0, prefix, a.window), kend = p0 + 1;
-    const int k0 = kbeg / KS * KS + c0 * GROUP;
-    const int k1 = kbeg < kend ? min(kend, kbeg / KS * KS + c1 * GROUP) : k0;  // none: no step
-    const int hq = h * a.G + q0 + min(lane & 15, rows - 1);
+    const int b0 = i0 + at, p = uniform(rows.prefix[at]);
+    // a row block: query heads rho0 .. rho0 + nrow - 1 of head h of the rows from
+    // b0 on, whose positions lie in [minpos, maxpos], against [k0, k1) of the keys
+    // [kbeg, kend) that count
+    int rho0 = 0, nrow, seq, h, minpos, maxpos, kbeg, kend, k0, k1;
+    if (shared) {
+      const bool tile = uniform(rows.tile[at]);
+      const int RT = block_rows(tile, a.G), L = uniform(rows.lead[at]);
+      seq = uniform(rows.lead_seq[at]);
+      h = j;
+      // its rows (up to RT of one group), and the positions they span
+      int cnt = 0;
+      for (int i = 0; i < RT && cnt == i; i += WAVE) {
+        const int b = min(b0 + i + lane, n - 1);
+        const int name = b < i0 + WAVE ? rows.name[b - i0] : x.lead[b];
+        const uint64_t out = ~__ballot(i + lane < RT && b0 + i + lane < n && name == L);
+        cnt = i + (out ? __ffsll((unsigned long long)out) - 1 : WAVE);
+      }
+      maxpos = -1;
+      minpos = FAR;
+      for (int i = 0; i < cnt; i += WAVE) {
+        const int p0 = i + lane < cnt ? row_p0(b0 + i + lane) : -1;
+        maxpos = max(maxpos, p0);
+        if (p0 >= 0) minpos = min(minpos, p0);
+      }
+      maxpos = uniform(lane_max(maxpos));
+      minpos = uniform(maxpos < 0 ? 0 : FAR - lane_max(FAR - minpos));
+      nrow = uniform(cnt) * a.G;
+      const int keys = tile ? TC::KB : GROUP;
+      kbeg = max(a.window && maxpos >= 0 ? minpos - a.window + 1 : 0, c0 * keys);
+      kend = min(min(p, maxpos + 1), c1 * keys);
+      if (kbeg >= kend) kbeg = kend = 0;
+      if constexpr (TILES) {
+        if (tile) {
+          // this lane's query; of a row that is not served nothing is made, and any
+          // position will do
+          const int wave = uniform(tid / WAVE), r = wave * 32 + (lane & 31);
+          const int rho = min(r, nrow - 1), b = b0 + rho / a.G, hq = h * a.G + rho % a.G;
+          const int p0 = row_p0(b);
+          const char* qp = a.q + (int64_t)b * a.q_stride + (int64_t)hq * a.D * W;
+          f32x16 o[TC::DT];
+          float m, l;
+          bool missing;
+          tile_keys<T, DP, FULL, E8, true>(tid, a, a.table + (int64_t)seq * a.M, h, kbeg, kend,
+                                           minpos, wave * 32 < nrow ? maxpos : -1, qp,
+                                           p0 < 0 ? maxpos : p0, lds, lds + TILE_LDS / 2, o, m, l,
+                                           missing);
+          if (missing && lane == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
+          l = swap32_add(l, l);
+          if (r < nrow) {
+            const int h2 = lane >> 5;
+            const int row = part_of(c0 == 0, 0, b, hq, r);
+#pragma unroll
+            for (int j = 0; j < TC::DT; ++j)
+#pragma unroll
+              for (int i = 0; i < 16; i += 4)
+                put(row, 32 * j + 2 * i + 4 * h2,
+                    make_float4(o[j][i], o[j][i + 1], o[j][i + 2], o[j][i + 3]));
+            if (h2 == 0) *(float2*)(a.ml + (size_t)row * 2) = make_float2(m, l);
+          }
+          return;
+        }
+      }
+      k0 = kbeg / KS * KS;
+      k1 = kend;
+    } else {
+      h = j % a.Hkv;
+      rho0 = j / a.Hkv * RB;
+      nrow = min(RB, a.G - rho0);
+      seq = uniform(rows.seq[at]);
+      minpos = maxpos = uniform(rows.p0[at]);
+      kbeg = own_first<KS>(maxpos, p, a.window);
+      kend = maxpos + 1;
+      k0 = kbeg / KS * KS + c0 * GROUP;
+      k1 = kbeg < kend ? min(kend, kbeg / KS * KS + c1 * GROUP) : k0;  // none: no step
+    }
+    const int rho = rho0 + min(lane & 15, nrow - 1), b = b0 + rho / a.G, hq = h * a.G + rho % a.G;
+    const int p0 = row_p0(b);
     f32x4 o[C::VS][C::NV];
     float m, l;
     bool missing;
-    rows_keys<T, DP, FULL, E8, true>(tid, a, a.table + (int64_t)seq * a.M, h, p0, p0, kbeg, kend, k0, k1,
-                               a.q + (int64_t)b * a.q_stride + (int64_t)hq * a.D * W, p0, o, m, l,
-                               missing);
+    rows_keys<T, DP, FULL, E8, true>(tid, a, a.table + (int64_t)seq * a.M, h, minpos, maxpos, kbeg,
+                                     kend, k0, k1,
+                                     a.q + (int64_t)b * a.q_stride + (int64_t)hq * a.D * W,
+                                     p0 < 0 ? maxpos : p0, o, m, l, missing);
     if (missing && lane == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
     rows_meet<C>(o, m, l, rl.o, rl.m, rl.l);
     __syncthreads();
-    for (int u = threadIdx.x; u < rows * (DP / 4); u += ROWS_T) {
+    for (int u = tid; u < nrow * (DP / 4); u += ROWS_T) {
       const int q = u / (DP / 4), d = u % (DP / 4) * 4;
       float M, L;
       const float4 sum = rows_met<C>(rl.o, rl.m, rl.l, q, d, M, L);
-      const int row = part_of(first, n * x.Hq, b, h * a.G + q0 + q, q);
+      const int row = part_of(c0 == 0, shared ? 0 : n * x.Hq, b0 + (rho0 + q) / a.G,
+                              h * a.G + (rho0 + q) % a.G, q);
       put(row, d, sum);
       if (d == 0) *(float2*)(a.ml + (size_t)row * 2) = make_float2(M, L);
     }
     __syncthreads();  // LDS is free again
   };
 
-  int pb = 0, sb = 0;  // units of the chunks before
+  int pb = 0, sb = tp;  // weights before the chunk
   run = 0;
-  for (int i0 = 0; i0 < n && (pb < s1 || sb < g1); i0 += WAVE) {
+  for (; i0 < n && (pb < min(tp, end) || sb < end); i0 += WAVE) {
     if (n > WAVE) {
       load(i0, run, nullptr);
       run = last(sr.run);
@@ -285,50 +308,48 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
       rows.steps[lane] = steps;
       rows.up_at[lane] = pb + up_at - up;
       rows.lead[lane] = sr.lead;
+      rows.name[lane] = sr.name;
       rows.prefix[lane] = sr.prefix;
       rows.lead_seq[lane] = sr.seq;
-      rows.us[lane] = us;
+      rows.tile[lane] = sr.tile;
+      rows.groups[lane] = groups;
       rows.us_at[lane] = sb + us_at - us;
       rows.p0[lane] = sr.row.p0;
       rows.seq[lane] = sr.row.seq;
     }
-    uint64_t tiles = __ballot(up > 0 && pb + up_at > s0 && pb + up_at - up < s1);
-    uint64_t own = __ballot(us > 0 && sb + us_at > g0 && sb + us_at - us < g1);
+    const uint64_t with_tiles = __ballot(up > 0 && pb + up_at > beg && pb + up_at - up < end);
+    const uint64_t with_own = __ballot(us > 0 && sb + us_at > beg && sb + us_at - us < end);
     pb += last(up_at);
     sb += last(us_at);
     __syncthreads();
-    while (tiles) {
-      const int l = __ffsll((unsigned long long)tiles) - 1;
-      tiles &= tiles - 1;
-      const int st = uniform(rows.steps[l]), at = uniform(rows.up_at[l]);
-      for (int h = max(0, s0 - at) / st; h < a.Hkv; ++h) {
-        const int x0 = at + h * st, c0 = max(s0, x0), c1 = min(s1, x0 + st);
-        if (c0 >= c1) break;
-        if (c0 == x0 && threadIdx.x == 0)
-          x.info_p[(i0 + l) * a.Hkv + h] = wg | (x0 + st - 1) * P::WEIGHT / share << 16;
-        shared_part(i0 + l, uniform(rows.lead[l]), uniform(rows.prefix[l]),
-                    uniform(rows.lead_seq[l]), h, c0 - x0, c1 - x0, c0 == x0);
-      }
-    }
-    while (own) {
-      const int l = __ffsll((unsigned long long)own) - 1;
-      own &= own - 1;
-      const int gr = uniform(rows.us[l]) / nb, at = uniform(rows.us_at[l]);
-      for (int j = max(0, g0 - at) / gr; j < nb; ++j) {
-        const int x0 = at + j * gr, c0 = max(g0, x0), c1 = min(g1, x0 + gr);
-        if (c0 >= c1) break;
-        if (c0 == x0 && threadIdx.x == 0)
-          x.info_s[(i0 + l) * nb + j] =
-              wg | (tp * P::WEIGHT + (x0 + gr - 1) * OWN_WEIGHT) / share << 16;
-        own_part(i0 + l, uniform(rows.p0[l]), uniform(rows.seq[l]), uniform(rows.prefix[l]), j,
-                 c0 - x0, c1 - x0, c0 == x0);
+    for (int kind = 0; kind < 2; ++kind) {
+      const bool shared = kind == 0;
+      uint64_t hit = shared ? with_tiles : with_own;
+      while (hit) {
+        const int at = __ffsll((unsigned long long)hit) - 1;
+        hit &= hit - 1;
+        // this row's blocks that have units in the stretch
+        const Cost c = x.cost(shared && uniform(rows.tile[at]));
+        const int units = uniform(shared ? rows.steps[at] : rows.groups[at]);
+        const int start = uniform(shared ? rows.up_at[at] : rows.us_at[at]);
+        const int count = shared ? a.Hkv : nb, len = c.block(units);
+        int32_t* const info = shared ? x.info_p : x.info_s;
+        for (int j = max(0, beg - start) / len; j < count; ++j) {
+          const int x0 = start + j * len;
+          if (x0 >= end) break;
+          const int c0 = min(units, c.unit(beg - x0)), c1 = min(units, c.unit(end - x0));
+          if (c0 >= c1) continue;
+          if (c0 == 0 && threadIdx.x == 0)
+            info[(i0 + at) * count + j] = wg | (x0 + c.place(units - 1)) / share << 16;
+          part(shared, at, j, c0, c1);
+        }
       }
     }
   }
 }
 
 // A wave per query head: its parts joined, in their order.
-template <class T, int DP, int ROWS>
+template <class T, int DP>
 __global__ __launch_bounds__(ROWS_T) void attn_shared_join_kernel(SharedArgs x) {
   constexpr int TD = DP / 4, SUB = WAVE / TD, W = 16 / T::V;
   const AttnArgs& a = x.a;
@@ -336,8 +357,9 @@ __global__ __launch_bounds__(ROWS_T) void attn_shared_join_kernel(SharedArgs x) 
   const int id = uniform((int)(blockIdx.x * (ROWS_T / WAVE) + threadIdx.x / WAVE));
   if (id >= x.n * x.Hq) return;
   const int b = id / x.Hq, hq = id % x.Hq, h = hq / a.G, g = hq % a.G;
-  const int per = (a.G + RB - 1) / RB, nb = per * a.Hkv, RT = ROWS / a.G;
-  const int L = load_scalar(x.row_lead, b);
+  const int per = (a.G + RB - 1) / RB, nb = per * a.Hkv;
+  const int named = load_scalar(x.row_lead, b), L = named >> 1;
+  const int RT = block_rows(named & 1, a.G);
   const int is = load_scalar(x.info_s, b * nb + g / RB * a.Hkv + h);
   const int b0 = L < 0 ? b : L + (b - L) / RT * RT;
   const int ip = L < 0 ? 0 : load_scalar(x.info_p, b0 * a.Hkv + h);
@@ -346,9 +368,9 @@ __global__ __launch_bounds__(ROWS_T) void attn_shared_join_kernel(SharedArgs x) 
   const int ns = (is >> 16) - (is & 0xFFFF) + 1;
   const int extra = 2 * x.n * x.Hq;
   auto part_row = [&](int c) {
-    if (c < np) return c ? extra + ((ip & 0xFFFF) + c) * ROWS + (b - b0) * a.G + g : id;
+    if (c < np) return c ? extra + ((ip & 0xFFFF) + c) * TB + (b - b0) * a.G + g : id;
     c -= np;
-    return c ? extra + ((is & 0xFFFF) + c) * ROWS + g % RB : x.n * x.Hq + id;
+    return c ? extra + ((is & 0xFFFF) + c) * TB + g % RB : x.n * x.Hq + id;
   };
   const int parts = np + ns;
   float M = -INFINITY;
@@ -402,7 +424,6 @@ __global__ __launch_bounds__(ROWS_T) void attn_shared_join_kernel(SharedArgs x) 
 
 template <class T, int DP, bool E8>
 hipError_t launch_shared(const SharedArgs& x, hipStream_t stream) {
-  using P = SharedCfg<T, DP, E8>;
   const dim3 grid(DP == 256 ? SH_WG / 2 : SH_WG), block(ROWS_T);
   if (x.a.D == DP)
     hipLaunchKernelGGL((attn_shared_kernel<T, DP, true, E8>), grid, block, 0, stream, x);
@@ -411,7 +432,7 @@ hipError_t launch_shared(const SharedArgs& x, hipStream_t stream) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const unsigned waves = (unsigned)(x.n * x.Hq);
-  hipLaunchKernelGGL((attn_shared_join_kernel<T, DP, P::ROWS>),
+  hipLaunchKernelGGL((attn_shared_join_kernel<T, DP>),
                      dim3((waves + ROWS_T / WAVE - 1) / (ROWS_T / WAVE)), block, 0, stream, x);
   return hipGetLastError();
 }
@@ -433,11 +454,29 @@ hipError_t launch_attn_shared(const np_kv_shape& s, int layer, const np_kv_batch
   const int64_t n = b.n_seq, heads = n * s.heads;
   SharedArgs x;
   x.a = attn_args(s, layer, b, table, q, q_stride, pool, scale, window, out, out_stride, ws);
-  // the line's length: at most a tile a row, and every row's own keys
-  const int64_t line = n * s.kv_heads * ((int64_t)sh.max_prefix / 32 + 8) +
-                       heads * ((int64_t)x.a.b.lim / 32 + 8);
-  if (sh.max_prefix == 0 || n < 2 || heads > KV_SHARED_HEADS || G > (dtype == NP_F32 ? RB : TB) ||
-      line >= ((int64_t)1 << 30))
+  // The line counts 32 keys of a tile's rows: a row block's 128 keys cost as much as
+  // a tile's 128 (its rows are fewer, but so are the keys in flight), and a tile's
+  // beginning and end as much as four to eight of its steps.  Us with tiles' beginning
+  // and step at 8, 2 / 0, 2 / 0, 4 / 32, 2: 32 rows of 32 heads over 8 in four groups
+  // behind up to 3000 keys 22.2 / 27.7 / 23.2 / 24.1, 48 rows of 64 over 8 behind 32768 in
+  // 8-bit elements 79.7 / 87.6 / 104.9 / 86.1.
+  x.tile = {8, s.head_dim > 128 ? 1 : 2};
+  x.own = {0, 4};
+  x.least = 4;
+  x.small = dtype == NP_F32 ? 0 : 32;
+  // the line's length: at most a block of shared keys a row, and every row's own
+  const int64_t line =
+      n * s.kv_heads * (((int64_t)sh.max_prefix / 32 + 1) * x.tile.w + x.tile.fix + x.own.fix) +
+      heads * (((int64_t)x.a.b.lim / GROUP + 2) * x.own.w + x.own.fix);
+  // What sharing saves is at most the prefix's bytes for all rows but one; the join,
+  // and the search for the groups, cost 4 us and 0.1 a row, about what 32 MB and 1
+  // MB a row take to read.  Us apart / shared (bf16, 32 heads over 8 of 128; the
+  // bytes in brackets): 2 rows behind 2048 keys 11 / 15 (8 MB), behind 8192 22 / 20 (34
+  // MB); 8 rows behind 512 9 / 15 (15 MB), behind 2048 18 / 16 (59 MB); 32 rows behind
+  // 512 18 / 20 (65 MB), behind 2048 33 / 23 (260 MB).
+  const int64_t saved = (n - 1) * sh.max_prefix * s.kv_heads * 2 * kv_row_bytes(s);
+  if (saved < (32 + n) * 1000000 || heads > KV_SHARED_HEADS ||
+      G > (dtype == NP_F32 ? RB : TB) || line >= ((int64_t)1 << 30))
     return launch_attn(s, layer, b, table, q, q_stride, pool, scale, window, out, out_stride, ws,
                        stream);
   KvScratch k;
@@ -447,7 +486,6 @@ hipError_t launch_attn_shared(const np_kv_shape& s, int layer, const np_kv_batch
   x.max_prefix = sh.max_prefix;
   x.Hq = s.heads;
   x.n = (int)n;
-  x.least = 8;
   x.info_p = k.shared_p;
   x.info_s = k.shared_s;
   x.row_lead = k.shared_lead;

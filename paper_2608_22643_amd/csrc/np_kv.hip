@@ -420,9 +420,10 @@ struct AppendArgs {
   // norms and 8-bit elements (kv_append_heads_kernel)
   bool norm;
   const char *wq, *wk;  // nullptr: ones
-  float eps;
-  int lanes;  // log2 of the lanes that share a head
-  int parts;  // workgroups of a token
+  float eps, inv_dim;  // 1 / D
+  int lanes;           // log2 of the lanes that share a head
+  int sets;            // that a token's heads come in
+  bool split;          // a workgroup for each four of them
   int top;    // the scale byte at which 256 2^(b - 127) leaves the type
 };
 
@@ -634,165 +635,271 @@ __device__ inline void to_elements(const float* f, int b, int top, uint32_t* out
   }
 }
 
+// The same of 16 bytes of w that are finite, under a scale that needs no limit:
+// the conversion divides by the scale and rounds once.
+template <class T>
+__device__ inline void to_elements_fast(uint4 x, float scale, uint32_t* out) {
+  typedef short s16x2 __attribute__((ext_vector_type(2)));
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  s16x2 r = {0, 0};
+  if constexpr (T::V == 4) {
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, __uint_as_float(w[0]), __uint_as_float(w[1]),
+                                                 scale, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, __uint_as_float(w[2]), __uint_as_float(w[3]),
+                                                 scale, true);
+    out[0] = __builtin_bit_cast(uint32_t, r);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      if constexpr (T::dtype == NP_F16) {
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, as_h2(w[2 * e]), scale, false);
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, as_h2(w[2 * e + 1]), scale, true);
+      } else {
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, as_b2(w[2 * e]), scale, false);
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, as_b2(w[2 * e + 1]), scale, true);
+      }
+      out[e] = __builtin_bit_cast(uint32_t, r);
+    }
+  }
+}
+
+// The largest magnitude in 16 bytes of w, as the bits of a w without its sign
+// (whose order is that of the magnitudes; infinities and NaN are past them all).
+template <class T>
+__device__ inline uint32_t largest_bits(uint4 x, uint32_t m) {
+  if constexpr (T::V == 4) {
+    const uint32_t s = 0x7FFFFFFFu;
+    return max(max(max(x.x & s, x.y & s), max(x.z & s, x.w & s)), m);
+  } else {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    auto mag = [](uint32_t u) { return __builtin_bit_cast(u16x2, u & 0x7FFF7FFFu); };
+    const u16x2 y = __builtin_elementwise_max(__builtin_elementwise_max(mag(x.x), mag(x.y)),
+                                              __builtin_elementwise_max(mag(x.z), mag(x.w)));
+    return max(max((uint32_t)y.x, (uint32_t)y.y), m);
+  }
+}
+
+// fp32 to w, 16 bytes of it
+template <class T>
+__device__ inline uint4 round_row(const float* f) {
+  if constexpr (T::V == 4) {
+    return pack_row<T>(f);
+  } else {
+    uint32_t u[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const f32x2_t v = {f[2 * e], f[2 * e + 1]};
+      if constexpr (T::dtype == NP_F16)
+        u[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, half2_t));
+      else
+        u[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf162_t));
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+  }
+}
+
 // np_kv_append_norm, and any append of 8-bit elements.  A head is shared by
-// 2^lanes neighbouring lanes, each with the unit of 16 or 2 x 16 bytes of
-// kv_append_kernel, so that the sum of squares and the largest magnitude are
-// reductions between lanes' registers; a workgroup has 256 >> lanes heads of a
-// token.  The heads are asked for before the token's place is looked up: their
-// addresses need only its number.
-template <class T, bool INTER, bool E8>
+// 2^lanes neighbouring lanes, so that its sum of squares and its largest magnitude
+// are reductions between lanes' registers.  A lane has NP pieces of 16 bytes: one
+// (rotary pairs that are neighbours, or none), or the two that turn into each
+// other (pairs i, i + R/2; behind the rotary part one).  A set is as many heads of
+// a token as a wave holds, all queries, all keys or all values, so that what a
+// wave does with them, and their addresses, are the same for its lanes.  The heads are
+// asked for before the token's place is looked up, and a set's before the one
+// before it is worked on: their addresses need only the token's number.
+template <class T, int NP, bool E8>
 __global__ __launch_bounds__(APP_T) void kv_append_heads_kernel(AppendArgs a) {
   constexpr int V = T::V;
   constexpr int W = 16 / V;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / WAVE);
+  const int lane = threadIdx.x % WAVE;
   const int id = grid_block();
-  const int t = id / a.parts;
+  int t = id, set = wave, sets = a.sets;
+  bool report = true;
+  if (a.split) {  // a workgroup for every four sets
+    const int groups = (a.sets + APP_T / WAVE - 1) / (APP_T / WAVE);
+    t = id / groups;
+    set += (id - t * groups) * (APP_T / WAVE);
+    report = id == t * groups;
+    sets = min(sets, set + 1);
+  }
   if (t >= a.b.n_tokens) return;
   const int chunks = a.D / V;
-  const int half = INTER ? 0 : a.R / 2 / V;  // pieces that have a partner
-  const int u = threadIdx.x & ((1 << a.lanes) - 1);
-  int h = ((id % a.parts) << (__builtin_ctz(APP_T) - a.lanes)) + ((int)threadIdx.x >> a.lanes);
-  const int kind = h < a.Hq ? 0 : h < a.Hq + a.Hkv ? 1 : 2;
-  const bool live = h < a.Hq + 2 * a.Hkv && u < chunks - half;
-  if (kind) h -= a.Hq + (kind - 1) * a.Hkv;
-  const bool pair = u < half;
+  const int half = NP == 2 ? a.R / 2 / V : 0;  // pieces that have a partner
+  const int u = lane & ((1 << a.lanes) - 1), hl = lane >> a.lanes;
+  const int per = 6 - a.lanes;  // log2 of a set's heads
+  const bool pair = NP == 2 && u < half;
   const int c0 = pair ? u : u + half, c1 = u + half;  // this lane's pieces, c1 only of pairs
+  const int sq = (a.Hq + (1 << per) - 1) >> per, sk = (a.Hkv + (1 << per) - 1) >> per;
 
-  uint4 xa = make_uint4(0, 0, 0, 0), xb = xa;
-  uint4 ga = xa, gb = xa;
-  const char* g = kind == 0 ? a.wq : kind == 1 ? a.wk : nullptr;
-  if (live) {
-    const char* src = kind == 0   ? a.q + t * a.q_stride
-                      : kind == 1 ? a.k + t * a.k_stride
-                                  : a.v + t * a.v_stride;
-    src += (size_t)h * a.D * W;
-    xa = *(const uint4*)(src + c0 * 16);
-    if (pair) xb = *(const uint4*)(src + c1 * 16);
-    if (g) {
-      ga = *(const uint4*)(g + c0 * 16);
-      if (pair) gb = *(const uint4*)(g + c1 * 16);
-    }
-  }
-
-  const TokenAt at = find_token(a.b, a.table, a.M, a.N, a.P, t, id % a.parts ? nullptr : a.err);
+  struct Heads {
+    int kind, h;  // 0, 1, 2: queries, keys, values; this lane's head
+    bool live;
+    uint4 x[NP], w[NP];  // it, and its norm's weights
+  };
+  auto load = [&](int set) {
+    Heads d;
+    d.kind = set < sq ? 0 : set < sq + sk ? 1 : 2;
+    d.h = ((set - (d.kind == 0 ? 0 : d.kind == 1 ? sq : sq + sk)) << per) + hl;
+    d.live = d.h < (d.kind ? a.Hkv : a.Hq) && u < chunks - half;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) d.x[p] = d.w[p] = make_uint4(0, 0, 0, 0);
+    auto from = [&](const char* heads, const char* g) {
+      if (!d.live) return;
+      const char* src = heads + d.h * a.D * W;
+      d.x[0] = *(const uint4*)(src + c0 * 16);
+      if (pair) d.x[NP - 1] = *(const uint4*)(src + c1 * 16);
+      if (g) {
+        d.w[0] = *(const uint4*)(g + c0 * 16);
+        if (pair) d.w[NP - 1] = *(const uint4*)(g + c1 * 16);
+      }
+    };
+    if (d.kind == 0) from(a.q + t * a.q_stride, a.wq);
+    else if (d.kind == 1) from(a.k + t * a.k_stride, a.wk);
+    else from(a.v + t * a.v_stride, nullptr);
+    return d;
+  };
+  Heads next;
+  if (set < sets) next = load(set);
+  const TokenAt at = find_token(a.b, a.table, a.M, a.N, a.P, t, report ? a.err : nullptr);
   if (at.what != TokenAt::HERE) return;
   if (a.R && at.pos >= a.max_pos) {
-    if (threadIdx.x == 0 && id % a.parts == 0) raise(a.err, NP_DEVERR_STATE);
+    if (threadIdx.x == 0 && report) raise(a.err, NP_DEVERR_STATE);
     return;
   }
-
-  float f[2 * V];
-  T::unpack(xa, f);
-  T::unpack(xb, f + V);
-  if (a.norm) {
-    // the mean square in fp32; where the sum would leave fp32's range, that of
-    // the head divided by a power of two next to its largest magnitude (or to
-    // eps's root), which every lane of a head finds alike
-    float ss = 0.f;
+  // this lane's angles, the same in every set
+  constexpr int NA = NP == 1 ? V / 2 : V;
+  float cs[NA], sn[NA];
+  const bool turns = a.R && (NP == 2 ? pair : c0 * V < a.R);
+  if (turns) {
+    const size_t first = (size_t)at.pos * (a.R / 2) + c0 * NA;
 #pragma unroll
-    for (int e = 0; e < 2 * V; ++e) ss = __builtin_fmaf(f[e], f[e], ss);
-    ss = reduce_lanes(ss, a.lanes, [](float x, float y) { return x + y; });
-    float mean = ss / (float)a.D + a.eps;
-    float r = mean > 0.f ? 1.f / sqrtf(mean) : 0.f;
-    float down = 1.f;
-    const bool far = !(ss < 1e36f) || mean < 1e-27f;
-    if (__any(kind < 2 && live && far)) {
-      float m = 0.f;
-#pragma unroll
-      for (int e = 0; e < 2 * V; ++e) m = finite_f32(f[e]) ? fmaxf(m, fabsf(f[e])) : m;
-      m = reduce_lanes(m, a.lanes, [](float x, float y) { return fmaxf(x, y); });
-      m = fmaxf(m, sqrtf(a.eps));
-      const int ex = min(max((int)(__float_as_uint(m) >> 23), 2), 252);
-      const float scale = scale_of_byte(254 - ex);
-      float s2 = 0.f;
-#pragma unroll
-      for (int e = 0; e < 2 * V; ++e) s2 = __builtin_fmaf(f[e] * scale, f[e] * scale, s2);
-      s2 = reduce_lanes(s2, a.lanes, [](float x, float y) { return x + y; });
-      if (far && m > 0.f) {
-        down = scale;
-        r = 1.f / sqrtf(s2 / (float)a.D + a.eps * scale * scale);
-      }
-    }
-    if (kind < 2) {
-      float w[2 * V];
-      T::unpack(ga, w);
-      T::unpack(gb, w + V);
-#pragma unroll
-      for (int e = 0; e < 2 * V; ++e) f[e] = f[e] * down * r * (g ? w[e] : 1.f);
+    for (int e = 0; e < NA; e += 2) {
+      *(float2*)&cs[e] = *(const float2*)(a.cos + first + e);
+      *(float2*)&sn[e] = *(const float2*)(a.sin + first + e);
     }
   }
-  const bool turned = kind < 2 && (INTER ? c0 * V < a.R : pair);
-  if (turned) {
-    const float* cs = a.cos + (size_t)at.pos * (a.R / 2);
-    const float* sn = a.sin + (size_t)at.pos * (a.R / 2);
-    float o[2 * V];
-    if constexpr (INTER) {
+  char* const page = a.pool + (size_t)at.page * a.page_bytes;
+  const int slot = at.pos % a.P;
+  const int head_bytes = a.P * (E8 ? a.D + 1 : a.D * W);  // of a page
+
+  auto add = [](float x, float y) { return x + y; };
+  auto most = [](float x, float y) { return fmaxf(x, y); };
+  for (; set < sets; set += APP_T / WAVE) {
+    Heads d = next;
+    if (set + APP_T / WAVE < sets) next = load(set + APP_T / WAVE);
+    if (d.kind < 2 && (a.norm || a.R)) {
+      float f[NP * V];
 #pragma unroll
-      for (int e = 0; e < V; e += 2) {
-        const float co = cs[(c0 * V + e) / 2], si = sn[(c0 * V + e) / 2];
-        o[e] = f[e] * co - f[e + 1] * si;
-        o[e + 1] = f[e + 1] * co + f[e] * si;
-        o[e + V] = o[e + V + 1] = 0.f;
-      }
-    } else {
+      for (int p = 0; p < NP; ++p) T::unpack(d.x[p], f + p * V);
+      if (a.norm) {
+        // the mean square in fp32; where the sum would leave fp32's range, that of
+        // the head divided by a power of two next to its largest magnitude (or to
+        // eps's root), which every lane of a head finds alike
+        float ss = 0.f;
 #pragma unroll
-      for (int e = 0; e < V; e += 4) {
-        const float4 co = *(const float4*)(cs + c0 * V + e), si = *(const float4*)(sn + c0 * V + e);
-        const float* cp = &co.x;
-        const float* sp = &si.x;
+        for (int p = 0; p < NP; ++p) ss = T::dot(d.x[p], d.x[p], ss);
+        ss = reduce_lanes(ss, a.lanes, add);
+        const float mean = ss * a.inv_dim + a.eps;
+        float r = mean > 0.f ? __builtin_amdgcn_rsqf(mean) : 0.f;
+        const bool far = !(ss < 1e36f) || mean < 1e-27f;
+        if (__any(d.live && far)) {
+          float m = 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          o[e + j] = f[e + j] * cp[j] - f[e + j + V] * sp[j];
-          o[e + j + V] = f[e + j + V] * cp[j] + f[e + j] * sp[j];
+          for (int e = 0; e < NP * V; ++e) m = finite_f32(f[e]) ? fmaxf(m, fabsf(f[e])) : m;
+          m = fmaxf(reduce_lanes(m, a.lanes, most), sqrtf(a.eps));
+          const int ex = min(max((int)(__float_as_uint(m) >> 23), 2), 252);
+          const float scale = scale_of_byte(254 - ex);
+          float s2 = 0.f;
+#pragma unroll
+          for (int e = 0; e < NP * V; ++e) s2 = __builtin_fmaf(f[e] * scale, f[e] * scale, s2);
+          s2 = reduce_lanes(s2, a.lanes, add);
+          if (far && m > 0.f) {
+            r = __builtin_amdgcn_rsqf(s2 * a.inv_dim + a.eps * scale * scale);
+#pragma unroll
+            for (int e = 0; e < NP * V; ++e) f[e] *= scale;
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < NP * V; ++e) f[e] *= r;
+        if (d.kind == 0 ? a.wq : a.wk) {
+          float w[V];
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            T::unpack(d.w[p], w);
+#pragma unroll
+            for (int e = 0; e < V; ++e) f[p * V + e] *= w[e];
+          }
         }
       }
+      if (turns)
+#pragma unroll
+        for (int e = 0; e < NA; ++e) {
+          const int i = NP == 1 ? 2 * e : e, j = NP == 1 ? 2 * e + 1 : e + V;
+          const float x = f[i], y = f[j];
+          f[i] = x * cs[e] - y * sn[e];
+          f[j] = y * cs[e] + x * sn[e];
+        }
+      if (a.norm || turns)  // the rounding to w
+#pragma unroll
+        for (int p = 0; p < NP; ++p) d.x[p] = round_row<T>(f + p * V);
     }
+    if (d.kind == 0 || !E8) {
+      char* dst = d.kind == 0
+                      ? a.q_out + t * a.q_out_stride
+                      : page + (d.kind == 1 ? 0 : (size_t)a.Hkv * head_bytes) + slot * a.D * W;
+      if (d.live) {
+        dst += (size_t)d.h * (d.kind == 0 ? a.D * W : head_bytes);
+        *(uint4*)(dst + c0 * 16) = d.x[0];
+        if (pair) *(uint4*)(dst + c1 * 16) = d.x[NP - 1];
+      }
+      continue;
+    }
+    if constexpr (E8) {
+      uint32_t bits = 0;
 #pragma unroll
-    for (int e = 0; e < 2 * V; ++e) f[e] = o[e];
-  }
-  if (kind < 2 && (a.norm || turned)) {  // the rounding to w
-    xa = pack_row<T>(f);
-    xb = pack_row<T>(f + V);
-  }
-  if (kind == 0 && live) {
-    char* dst = a.q_out + t * a.q_out_stride + (size_t)h * a.D * W;
-    *(uint4*)(dst + c0 * 16) = xa;
-    if (pair) *(uint4*)(dst + c1 * 16) = xb;
-  }
-  const int blk = (kind == 2 ? a.Hkv : 0) + h;  // of the page
-  const int slot = at.pos % a.P;
-  char* page = a.pool + (size_t)at.page * a.page_bytes;
-  if constexpr (!E8) {
-    if (!live || kind == 0) return;
-    char* dst = page + ((size_t)blk * a.P + slot) * a.D * W;
-    *(uint4*)(dst + c0 * 16) = xa;
-    if (pair) *(uint4*)(dst + c1 * 16) = xb;
-  } else {
-    // every lane takes part in the reduction, those of queries among them
-    T::unpack(xa, f);
-    T::unpack(xb, f + V);
-    float m = 0.f;
+      for (int p = 0; p < NP; ++p) bits = largest_bits<T>(d.x[p], bits);
+      float m;
+      if constexpr (V == 4) m = __uint_as_float(bits);
+      else m = T::lo(bits);
+      m = reduce_lanes(m, a.lanes, [](float x, float y) {  // NaN and infinity stay so
+        return __uint_as_float(max(__float_as_uint(x), __float_as_uint(y)));
+      });
+      int b = scale_byte(m);
+      uint32_t el[NP][V / 4];
+      if (__any(d.live && (!finite_f32(m) || b >= a.top))) {
+        float f[NP * V];
 #pragma unroll
-    for (int e = 0; e < 2 * V; ++e) m = finite_f32(f[e]) ? fmaxf(m, fabsf(f[e])) : m;
-    m = reduce_lanes(m, a.lanes, [](float x, float y) { return fmaxf(x, y); });
-    if (!live || kind == 0) return;
-    const int b = scale_byte(m);
-    char* dst = page + (size_t)blk * a.P * (a.D + 1);
-    uint32_t ea[V / 4], eb[V / 4];
-    to_elements<V>(f, b, a.top, ea);
-    to_elements<V>(f + V, b, a.top, eb);
-    auto put = [&](int c, const uint32_t* e) {
-      char* p = dst + slot * a.D + c * V;
-      if constexpr (V == 8) *(uint2*)p = make_uint2(e[0], e[1]);
-      else *(uint32_t*)p = e[0];
-    };
-    put(c0, ea);
-    if (pair) put(c1, eb);
-    if (u == 0) dst[a.P * a.D + slot] = (char)b;
+        for (int p = 0; p < NP; ++p) T::unpack(d.x[p], f + p * V);
+        m = 0.f;
+#pragma unroll
+        for (int e = 0; e < NP * V; ++e) m = finite_f32(f[e]) ? fmaxf(m, fabsf(f[e])) : m;
+        b = scale_byte(reduce_lanes(m, a.lanes, most));
+#pragma unroll
+        for (int p = 0; p < NP; ++p) to_elements<V>(f + p * V, b, a.top, el[p]);
+      } else {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) to_elements_fast<T>(d.x[p], scale_of_byte(b), el[p]);
+      }
+      if (d.live) {
+        char* dst = page + (d.kind == 1 ? 0 : (size_t)a.Hkv * head_bytes) +
+                    (size_t)d.h * head_bytes;
+        auto put = [&](int c, const uint32_t* e) {
+          char* p = dst + slot * a.D + c * V;
+          if constexpr (V == 8) *(uint2*)p = make_uint2(e[0], e[1]);
+          else *(uint32_t*)p = e[0];
+        };
+        put(c0, el[0]);
+        if (pair) put(c1, el[NP - 1]);
+        if (u == 0) dst[a.P * a.D + slot] = (char)b;
+      }
+    }
   }
 }
 
 // ---------------------------------------------------------------------------
-// np_kv_read: pieces of 16 bytes of a token's keys and values, a thread each.
+// np_kv_read: pieces of 16 bytes of a token's keys and values, NB of them a
+// thread, all asked for before the first is stored.
 // ---------------------------------------------------------------------------
 struct ReadArgs {
   KvBatch b;
@@ -801,49 +908,73 @@ struct ReadArgs {
   char *k, *v;
   int64_t k_stride, v_stride;  // bytes
   size_t page_bytes;
-  int Hkv, D, P, M, N, parts;
+  int Hkv, D, P, M, N, parts;  // parts: workgroups of a token
   int32_t* err;
 };
 
-template <class T, bool E8>
+template <class T, bool E8, int NB>
 __global__ __launch_bounds__(APP_T) void kv_read_kernel(ReadArgs a) {
-  constexpr int V = T::V;
+  constexpr int V = T::V, W = 16 / V;
   const int id = grid_block();
-  const int t = id / a.parts, part = id % a.parts;
+  int t = id, part = 0;
+  if (a.parts > 1) {
+    t = id / a.parts;
+    part = id - t * a.parts;
+  }
   if (t >= a.b.n_tokens) return;
   const TokenAt at = find_token(a.b, a.table, a.M, a.N, a.P, t, part ? nullptr : a.err);
   if (at.what == TokenAt::NOBODYS) return;
   const int chunks = a.D / V, n = a.Hkv * chunks;
-  int c = part * APP_T + (int)threadIdx.x;
-  const bool value = c >= n;
-  if (value) c -= n;
-  char* out = value ? a.v : a.k;
-  if (c >= n || !out) return;
-  out += t * (value ? a.v_stride : a.k_stride) + (int64_t)c * 16;
-  uint4 x = make_uint4(0, 0, 0, 0);
-  if (at.what == TokenAt::HERE) {
-    const int h = c / chunks, slot = at.pos % a.P;
+  const int slot = at.pos % a.P, head_bytes = a.P * (E8 ? a.D + 1 : a.D * W);
+  const char* page = a.pool + (size_t)at.page * a.page_bytes;
+  char* const k_out = a.k ? a.k + t * a.k_stride : nullptr;
+  char* const v_out = a.v ? a.v + t * a.v_stride : nullptr;
+  char* out[NB];
+  uint4 x[NB];
+  float s[NB];
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    int c = (part * NB + i) * APP_T + (int)threadIdx.x;
+    const bool value = c >= n;
+    if (value) c -= n;
+    out[i] = value ? v_out : k_out;
+    if (c >= n) out[i] = nullptr;
+    x[i] = make_uint4(0, 0, 0, 0);
+    s[i] = 1.f;
+    if (!out[i]) continue;
+    out[i] += c * 16;
+    if (at.what != TokenAt::HERE) continue;
+    const int h = c / chunks;
     c -= h * chunks;
-    const char* page = a.pool + (size_t)at.page * a.page_bytes;
-    const int blk = (value ? a.Hkv : 0) + h;
+    const char* head = page + (size_t)((value ? a.Hkv : 0) + h) * head_bytes;
     if constexpr (!E8) {
-      x = *(const uint4*)(page + (((size_t)blk * a.P + slot) * a.D + c * V) * (16 / V));
+      x[i] = *(const uint4*)(head + (slot * a.D + c * V) * W);
     } else {
-      const char* row = page + (size_t)blk * a.P * (a.D + 1);
-      const float s = scale_of_byte((uint8_t)row[a.P * a.D + slot]);
+      s[i] = scale_of_byte((uint8_t)head[a.P * a.D + slot]);
       if constexpr (V == 8) {
-        const uint2 e = *(const uint2*)(row + slot * a.D + c * V);
-        x = make_uint4(element_pair<T>(e.x, s, false), element_pair<T>(e.x, s, true),
-                       element_pair<T>(e.y, s, false), element_pair<T>(e.y, s, true));
+        const uint2 e = *(const uint2*)(head + slot * a.D + c * V);
+        x[i].x = e.x;
+        x[i].y = e.y;
       } else {
-        const f32x2_t lo = element_pair_f32(*(const uint32_t*)(row + slot * a.D + c * V), s, false);
-        const f32x2_t hi = element_pair_f32(*(const uint32_t*)(row + slot * a.D + c * V), s, true);
-        x = make_uint4(__float_as_uint(lo.x), __float_as_uint(lo.y), __float_as_uint(hi.x),
-                       __float_as_uint(hi.y));
+        x[i].x = *(const uint32_t*)(head + slot * a.D + c * V);
       }
     }
   }
-  *(uint4*)out = x;
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    if (!out[i]) continue;
+    uint4 y = x[i];
+    if constexpr (E8 && V == 8)
+      y = make_uint4(element_pair<T>(x[i].x, s[i], false), element_pair<T>(x[i].x, s[i], true),
+                     element_pair<T>(x[i].y, s[i], false), element_pair<T>(x[i].y, s[i], true));
+    if constexpr (E8 && V == 4) {
+      const f32x2_t lo = element_pair_f32(x[i].x, s[i], false);
+      const f32x2_t hi = element_pair_f32(x[i].x, s[i], true);
+      y = make_uint4(__float_as_uint(lo.x), __float_as_uint(lo.y), __float_as_uint(hi.x),
+                     __float_as_uint(hi.y));
+    }
+    *(uint4*)out[i] = y;
+  }
 }
 
 }  // namespace
@@ -973,23 +1104,27 @@ hipError_t launch_kv_append(const np_kv_shape& s, int layer, const np_kv_batch& 
   a.wq = norm ? (const char*)norm->q_weight : nullptr;
   a.wk = norm ? (const char*)norm->k_weight : nullptr;
   a.eps = norm ? norm->eps : 0.f;
+  a.inv_dim = 1.f / (float)a.D;
   a.top = dtype == NP_F16 ? 127 + 8 : 127 + 120;
-  const int v = vec_elems(dtype), units = a.D / v - (inter ? 0 : a.R / 2 / v);
+  const bool pairs = a.R && !inter;
+  const int v = vec_elems(dtype), units = a.D / v - (pairs ? a.R / 2 / v : 0);
   a.lanes = 0;
   while (1 << a.lanes < units) ++a.lanes;
-  const int per = APP_T >> a.lanes;  // heads of a workgroup
-  a.parts = (s.heads + 2 * s.kv_heads + per - 1) / per;
+  const int per = WAVE >> a.lanes;
+  a.sets = (s.heads + per - 1) / per + 2 * ((s.kv_heads + per - 1) / per);
+  const int groups = (a.sets + APP_T / WAVE - 1) / (APP_T / WAVE);
+  a.split = (int64_t)b.n_tokens * groups <= 2048;
   auto go = [&](auto kernel, int64_t blocks) {
     hipLaunchKernelGGL(kernel, block_grid(blocks), dim3(APP_T), 0, stream, a);
   };
   auto of = [&](auto t) {
     using T = decltype(t);
-    const int64_t n = b.n_tokens, parts = n * a.parts;
+    const int64_t n = b.n_tokens, wgs = a.split ? n * groups : n;
     if (!heads) inter ? go(kv_append_kernel<T, true>, n) : go(kv_append_kernel<T, false>, n);
-    else if (e8) inter ? go(kv_append_heads_kernel<T, true, true>, parts)
-                       : go(kv_append_heads_kernel<T, false, true>, parts);
-    else inter ? go(kv_append_heads_kernel<T, true, false>, parts)
-               : go(kv_append_heads_kernel<T, false, false>, parts);
+    else if (e8) pairs ? go(kv_append_heads_kernel<T, 2, true>, wgs)
+                       : go(kv_append_heads_kernel<T, 1, true>, wgs);
+    else pairs ? go(kv_append_heads_kernel<T, 2, false>, wgs)
+               : go(kv_append_heads_kernel<T, 1, false>, wgs);
   };
   if (dtype == NP_F32) of(TF32{});
   else if (dtype == NP_F16) of(TF16{});
@@ -1017,7 +1152,9 @@ hipError_t launch_kv_read(const np_kv_shape& s, int layer, const np_kv_batch& b,
   a.P = s.page_size;
   a.M = s.seq_pages;
   a.N = s.n_pages;
-  a.parts = (2 * s.kv_heads * (s.head_dim / vec_elems(dtype)) + APP_T - 1) / APP_T;
+  const int pieces = 2 * s.kv_heads * (s.head_dim / vec_elems(dtype));
+  const bool many = pieces > 2 * APP_T && (int64_t)b.n_tokens * pieces > 2048 * APP_T;
+  a.parts = (pieces + APP_T * (many ? 4 : 1) - 1) / (APP_T * (many ? 4 : 1));
   a.err = (int32_t*)((char*)ws + WS_ERR);
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, block_grid((int64_t)b.n_tokens * a.parts), dim3(APP_T), 0, stream,
@@ -1025,8 +1162,8 @@ hipError_t launch_kv_read(const np_kv_shape& s, int layer, const np_kv_batch& b,
   };
   auto of = [&](auto t) {
     using T = decltype(t);
-    if (kv_e4m3(s)) go(kv_read_kernel<T, true>);
-    else go(kv_read_kernel<T, false>);
+    if (kv_e4m3(s)) many ? go(kv_read_kernel<T, true, 4>) : go(kv_read_kernel<T, true, 1>);
+    else many ? go(kv_read_kernel<T, false, 4>) : go(kv_read_kernel<T, false, 1>);
   };
   if (dtype == NP_F32) of(TF32{});
   else if (dtype == NP_F16) of(TF16{});

@@ -95,9 +95,14 @@ class Setup:
         a = dict(n_seq=self.n, n_tokens=self.n, max_tokens=1, max_len=self.max_len, pos0=i32(self.pos))
         return B.make_kv_batch(**dict(a, **kw))
 
+    def bound(self):
+        """A max_prefix that lets sharing look worth while, so that small cases take its kernels too."""
+        row = self.D if self.shape.dtype & B.NP_KV_E4M3 else self.D * DT[self.dtype].itemsize
+        return max(max(self.prefix), (32 + self.n) * 1000000 // max(1, (self.n - 1) * self.Hkv * 2 * row) + 1)
+
     def shared(self, lead=None, prefix=None, most=None):
         return B.make_kv_shared(i32(self.lead if lead is None else lead), i32(self.prefix if prefix is None else prefix),
-                                max(self.prefix) if most is None else most)
+                                self.bound() if most is None else most)
 
     def run(self, shared=None, window=0, batch=None, table=None, out=None, q=None):
         out = torch.full(self.q.shape, 7.0, dtype=self.q.dtype, device=DEV) if out is None else out
@@ -205,12 +210,12 @@ def test_agrees_with_decode(dtype):
     ([0, 1, 0, 3, 3], None, [2]),                # not next to each other
     ([0, 0, 0, 3, 1 << 30], None, [4]),
     (None, [-1, 100, 100, 70, 70], [0, 1, 2]),   # a prefix below 0
-    (None, [100, 7, 9, 101, 70], [3, 4]),        # past max_prefix
+    (None, [100, 7, 9, 1 << 30, 70], [3, 4]),    # past max_prefix
 ])
 def test_bad_leads(dtype, lead, prefix, bad):
     """Rows with a bad lead are computed by themselves, and the error bit is set."""
     s = Setup([(100, [1, 5, 30]), (70, [2, 9])], 4, 2, 64, 16, dtype, seed=13)
-    out = s.run(s.shared(lead, prefix, most=100))
+    out = s.run(s.shared(lead, prefix))
     s.check(out)
     assert bad and s.error() == B.NP_DEVERR_STATE
 
@@ -251,7 +256,7 @@ def test_rows_name_their_sequences():
     out = torch.zeros(4, 4, 64, dtype=torch.bfloat16, device=DEV)
     batch = B.make_kv_batch(4, 4, 1, s.max_len, i32([s.pos[b] for b in pick]), seqs=i32(pick))
     # row 1 of the first group has its own copy of the prefix's last page
-    shared = B.make_kv_shared(i32([0, 0, 2, 2]), i32([70, 0, 100, 0]), 100)
+    shared = B.make_kv_shared(i32([0, 0, 2, 2]), i32([70, 0, 100, 0]), 2 * s.bound())
     B.np_attn_decode_shared(s.shape, 0, batch, shared, s.table.to(DEV), s.qd[pick].contiguous(), s.pool, s.scale, 0, out,
                             s.ws)
     whole = torch.zeros_like(s.q)
@@ -287,6 +292,7 @@ def test_values_that_are_not_finite(dtype):
 def test_batches_past_the_parts():
     """More query heads than have rows in the workspace: np_attn_decode's results."""
     s = Setup([(40, [1] * 500), (9, [3] * 20)], 64, 8, 16, 16, "f16", seed=19)
+    assert s.n * s.Hq > 32768
     plain = torch.zeros_like(s.qd)
     B.np_attn_decode(s.shape, 0, s.batch(), s.table.to(DEV), s.qd, s.pool, s.scale, 0, plain, s.ws)
     assert torch.equal(s.run(), plain.cpu())
@@ -301,9 +307,9 @@ def test_batches_up_to_the_parts():
 
 @pytest.mark.parametrize("loose", [False, True])
 def test_bounds_only_bound(loose):
-    """max_len and max_prefix far past what the rows have."""
+    """max_len and max_prefix far past what the rows have; as tight as they go, the keys are read row by row."""
     s = Setup(GROUPS[2], 8, 2, 64, 16, "bf16", seed=21)
-    s.check(s.run(s.shared(most=1 << 20 if loose else None), batch=s.batch(max_len=s.M * 16 if loose else s.max_len)))
+    s.check(s.run(s.shared(most=1 << 20 if loose else 200), batch=s.batch(max_len=s.M * 16 if loose else s.max_len)))
 
 
 @pytest.mark.parametrize("cache", ["same", "e4m3"])
@@ -312,7 +318,7 @@ def test_graph_replays(cache):
     s = Setup([(200, [40, 9, 30]), (70, [20, 9])], 8, 2, 128, 16, "bf16", cache, seed=22)
     pos, lead, prefix, table = i32(s.pos), i32(s.lead), i32(s.prefix), s.table.to(DEV)
     out = torch.zeros_like(s.qd)
-    batch, shared = s.batch(pos0=pos), B.make_kv_shared(lead, prefix, 200)
+    batch, shared = s.batch(pos0=pos), B.make_kv_shared(lead, prefix, s.bound())
 
     def call(stream=None):
         B.np_attn_decode_shared(s.shape, 0, batch, shared, table, s.qd, s.pool, s.scale, 0, out, s.ws, stream)

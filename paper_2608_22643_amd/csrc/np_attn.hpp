@@ -288,11 +288,14 @@ struct RowsCfg {
 // Each wave takes every fourth step, and has its own maximum m, sum l and
 // outputs o afterwards; missing: a key had no page.
 // CUT: the rows may see keys before kbeg or from kend on, which other stretches have.
-template <class T, int DP, bool FULL, bool E8, bool CUT, class C = RowsCfg<T, DP, E8>>
+// QT: blocks of 16 rows at once, each with its own queries and results; the keys
+// and values are loaded, and turned into operands, for all of them together.
+template <class T, int DP, bool FULL, bool E8, bool CUT, int QT, class C = RowsCfg<T, DP, E8>>
 __device__ __forceinline__ void rows_keys(int tid, const AttnArgs& a, const int32_t* trow, int h,
                                           int minpos, int maxpos, int kbeg, int kend, int k0, int k1,
-                                          const char* qp, int qpos, f32x4 (&o)[C::VS][C::NV],
-                                          float& m, float& l, bool& missing) {
+                                          const char* const (&qp)[QT], const int (&qpos)[QT],
+                                          f32x4 (&o)[QT][C::VS][C::NV], float (&m)[QT],
+                                          float (&l)[QT], bool& missing) {
   constexpr int V = C::V, W = C::W, KS = C::KS, KT = C::KT, KD = C::KD, KP = C::KP, NS = C::NS,
                 NV = C::NV, VS = C::VS, VR = C::VR;
   const int lane = tid % WAVE;
@@ -300,8 +303,12 @@ __device__ __forceinline__ void rows_keys(int tid, const AttnArgs& a, const int3
   const int r = lane & 15, g = lane >> 4;
   const int klast = max(kend - 1, 0);
   // the keys that this lane's query counts
-  const int klast_seen = CUT ? min(qpos, kend - 1) : qpos;
-  const int kfirst_seen = max(a.window ? qpos - a.window + 1 : 0, CUT ? kbeg : 0);
+  int klast_seen[QT], kfirst_seen[QT];
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    klast_seen[x] = CUT ? min(qpos[x], kend - 1) : qpos[x];
+    kfirst_seen[x] = max(a.window ? qpos[x] - a.window + 1 : 0, CUT ? kbeg : 0);
+  }
   // page ids through the scalar cache.  A step of 32 keys has two pages when
   // P is 16.
   struct Pages {
@@ -317,18 +324,21 @@ __device__ __forceinline__ void rows_keys(int tid, const AttnArgs& a, const int3
   Pages pg = {0, 0};
   if (base < k1) pg = pages_of(base);
   // this lane's query (B operand): column r
-  uint4 qf[KD];
+  uint4 qf[QT][KD];
 #pragma unroll
-  for (int s = 0; s < KD; ++s) {
-    const int d = C::kdim(s, g);
-    qf[s] = FULL || d < a.D ? *(const uint4*)(qp + d * W) : make_uint4(0, 0, 0, 0);
+  for (int x = 0; x < QT; ++x) {
+#pragma unroll
+    for (int s = 0; s < KD; ++s) {
+      const int d = C::kdim(s, g);
+      qf[x][s] = FULL || d < a.D ? *(const uint4*)(qp[x] + d * W) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int s = 0; s < VS; ++s)
+#pragma unroll
+      for (int j = 0; j < NV; ++j) o[x][s][j] = (f32x4)(0.f);
+    m[x] = -INFINITY;
+    l[x] = 0.f;
   }
-#pragma unroll
-  for (int s = 0; s < VS; ++s)
-#pragma unroll
-    for (int j = 0; j < NV; ++j) o[s][j] = (f32x4)(0.f);
-  m = -INFINITY;
-  l = 0.f;
 
   const int P1 = (1 << a.pshift) - 1;
   constexpr int EW = E8 ? 1 : W;  // bytes of an element of the cache
@@ -435,17 +445,19 @@ __device__ __forceinline__ void rows_keys(int tid, const AttnArgs& a, const int3
     const bool full = ok == 3 && base + KS - 1 <= minpos &&
                       (a.window == 0 || base > maxpos - a.window) &&
                       (!CUT || (base >= kbeg && base + KS <= kend));
-    f32x4 sc[KT];
+    f32x4 sc[QT][KT];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
-      sc[kt] = (f32x4)(0.f);
+#pragma unroll
+      for (int x = 0; x < QT; ++x) sc[x][kt] = (f32x4)(0.f);
 #pragma unroll
       for (int s = 0; s < KD; ++s) {
         u32x4_t k;
         if constexpr (E8) k = elements16<T>(kf[kt][s / NS], s % NS, scale_of_byte(ks[kt]));
         else k = kf[kt][s];
         if (!FULL && C::kdim(s, g) >= a.D) k = (u32x4_t)(0u);
-        sc[kt] = mfma_step<T>(as_uint4(k), qf[s], sc[kt]);
+#pragma unroll
+        for (int x = 0; x < QT; ++x) sc[x][kt] = mfma_step<T>(as_uint4(k), qf[x][s], sc[x][kt]);
       }
     }
     if constexpr (!LAST) {
@@ -455,51 +467,54 @@ __device__ __forceinline__ void rows_keys(int tid, const AttnArgs& a, const int3
       load_k(next, pg);
       pg = pages_of(next + NWAVE * KS);
     }
-    // scores of key base + vk + 4 kt + i
-    float p[4 * KT];
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) p[4 * kt + i] = sc[kt][i] * a.scale;
     const bool has = (ok >> (KS == 32 && g >= 2 ? 1 : 0)) & 1;
-    if (!full) {
+    uint4 pb[QT];
+#pragma unroll
+    for (int x = 0; x < QT; ++x) {
+      // scores of key base + vk + 4 kt + i
+      float p[4 * KT];
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[4 * kt + i] = sc[x][kt][i] * a.scale;
+      if (!full) {
+#pragma unroll
+        for (int i = 0; i < 4 * KT; ++i) {
+          const int key = base + vk + i;
+          if (!has || key > klast_seen[x] || key < kfirst_seen[x]) p[i] = -INFINITY;
+        }
+      }
+      float mx = p[0];
+#pragma unroll
+      for (int i = 1; i < 4 * KT; ++i) mx = fmaxf(mx, p[i]);
+      mx = max_groups(mx);
+      if (__any(mx > m[x])) {
+        const float mn = fmaxf(m[x], mx);
+        const float alpha = m[x] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[x] - mn);
+        m[x] = mn;
+        l[x] *= alpha;
+#pragma unroll
+        for (int s = 0; s < VS; ++s)
+#pragma unroll
+          for (int j = 0; j < NV; ++j) o[x][s][j] *= alpha;
+      }
+      const float mu = m[x] == -INFINITY ? 0.f : m[x];  // nothing visible yet: 2^(-inf) = 0
 #pragma unroll
       for (int i = 0; i < 4 * KT; ++i) {
-        const int key = base + vk + i;
-        if (!has || key > klast_seen || key < kfirst_seen) p[i] = -INFINITY;
+        p[i] = __builtin_amdgcn_exp2f(p[i] - mu);
+        l[x] += p[i];
       }
-    }
-    float mx = p[0];
-#pragma unroll
-    for (int i = 1; i < 4 * KT; ++i) mx = fmaxf(mx, p[i]);
-    mx = max_groups(mx);
-    if (__any(mx > m)) {
-      const float mn = fmaxf(m, mx);
-      const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-      m = mn;
-      l *= alpha;
-#pragma unroll
-      for (int s = 0; s < VS; ++s)
-#pragma unroll
-        for (int j = 0; j < NV; ++j) o[s][j] *= alpha;
-    }
-    const float mu = m == -INFINITY ? 0.f : m;  // nothing visible yet: 2^(-inf) = 0
-#pragma unroll
-    for (int i = 0; i < 4 * KT; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(p[i] - mu);
-      l += p[i];
-    }
-    uint4 pb;
-    if constexpr (V == 8) {
-      // rounded to the type of V, as the matrix cores take it; the sum l
-      // keeps the unrounded values
-      pb.x = pack2<T>(p[0], p[1]);
-      pb.y = pack2<T>(p[2], p[3]);
-      pb.z = pack2<T>(p[4], p[5]);
-      pb.w = pack2<T>(p[6], p[7]);
-    } else {
-      pb = make_uint4(__float_as_uint(p[0]), __float_as_uint(p[1]), __float_as_uint(p[2]),
-                      __float_as_uint(p[3]));
+      if constexpr (V == 8) {
+        // rounded to the type of V, as the matrix cores take it; the sum l
+        // keeps the unrounded values
+        pb[x].x = pack2<T>(p[0], p[1]);
+        pb[x].y = pack2<T>(p[2], p[3]);
+        pb[x].z = pack2<T>(p[4], p[5]);
+        pb[x].w = pack2<T>(p[6], p[7]);
+      } else {
+        pb[x] = make_uint4(__float_as_uint(p[0]), __float_as_uint(p[1]), __float_as_uint(p[2]),
+                           __float_as_uint(p[3]));
+      }
     }
     __builtin_amdgcn_sched_barrier(0);
     float f[VR];
@@ -540,7 +555,8 @@ __device__ __forceinline__ void rows_keys(int tid, const AttnArgs& a, const int3
         } else {
           av = make_uint4(vf[0][s][j], vf[1][s][j], vf[2][s][j], vf[3][s][j]);
         }
-        o[s][j] = mfma_step<T>(av, pb, o[s][j]);
+#pragma unroll
+        for (int x = 0; x < QT; ++x) o[x][s][j] = mfma_step<T>(av, pb[x], o[x][s][j]);
       }
     }
     if constexpr (!LAST) {
@@ -639,17 +655,19 @@ __global__ __launch_bounds__(ROWS_T, DP < 256 ? (E8 ? 3 : 2) : E8 ? 2 : 1) void 
   const int rr = min(r, t.nrow - 1);
   const int tok = (t.rho0 + rr) / a.G, head = h * a.G + (t.rho0 + rr) % a.G;
   const int qpos = t.row.p0 + tok;
-  f32x4 o[VS][NV];
-  float m, l;
+  f32x4 o[1][VS][NV];
+  float m[1], l[1];
   bool missing;
-  rows_keys<T, DP, FULL, E8, false>(
-      threadIdx.x, a, a.table + (int64_t)t.row.seq * a.M, h, t.minpos, t.maxpos, kbeg, kend, k0, k1,
-      a.q + (int64_t)(t.row.begin + tok) * a.q_stride + (int64_t)head * a.D * W, qpos, o, m, l,
-      missing);
+  const char* const qp[1] = {a.q + (int64_t)(t.row.begin + tok) * a.q_stride +
+                             (int64_t)head * a.D * W};
+  const int qps[1] = {qpos};
+  rows_keys<T, DP, FULL, E8, false, 1>(threadIdx.x, a, a.table + (int64_t)t.row.seq * a.M, h,
+                                       t.minpos, t.maxpos, kbeg, kend, k0, k1, qp, qps, o, m, l,
+                                       missing);
   if (missing && lane == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
 
   // the four waves' results meet in LDS
-  rows_meet<C>(o, m, l, s_o, s_m, s_l);
+  rows_meet<C>(o[0], m[0], l[0], s_o, s_m, s_l);
   __syncthreads();
   auto store_out = [&](int qr, int d, float4 sum, float L) {
     const float inv = 1.f / L;

@@ -59,6 +59,18 @@ __device__ inline KvRow lane_row(const KvBatch& b, int i, int32_t* err) {
   return kv_row_check(b, {i, i + 1, b.seqs ? b.seqs[i] : i, b.pos0[i]}, err);
 }
 
+// What a group's shared keys are computed in: row blocks, two of them side by side
+// (the keys loaded once for both), or tiles.  Two side by side pay where the keys are
+// bound by memory and not by one unit's latency (us, one block after the other / side
+// by side: 8 rows of 32 heads over 8 behind 2048 keys 16.0 / 19.3, behind 8192 25.5 / 24.4,
+// behind 32768 53 / 41; 32 rows of 32 over 32 behind 8192 59 / 43), and never in fp32, which
+// the products bound (32 rows of 4 over 4: 15.0 / 19.2, 20.5 / 22.4, 34 / 34).
+enum { BLOCK, TWO_BLOCKS, TILE };
+constexpr int SIDE_BY_SIDE = 65536;  // keys of all heads from which on
+__device__ inline int kind_rows(int kind) {
+  return kind == TILE ? TB : kind == TWO_BLOCKS ? 2 * RB : RB;
+}
+
 // Rows i0 .. i0 + 63, one a lane.
 struct SharedRow {
   KvRow row;
@@ -67,8 +79,9 @@ struct SharedRow {
   int seq;     // the lead's sequence
   int run;     // the first of the neighbouring rows that name the same lead
   int name;    // the lead that the row names
-  bool tile;   // the group's blocks are tiles
+  int kind;    // what the group's shared keys are computed in
 };
+template <bool TILES>
 __device__ inline SharedRow shared_row(const SharedArgs& x, int i0, int run_before, int32_t* err) {
   const int lane = threadIdx.x % WAVE, n = x.n;
   const int i = min(i0 + lane, n - 1);
@@ -84,7 +97,9 @@ __device__ inline SharedRow shared_row(const SharedArgs& x, int i0, int run_befo
   s.seq = x.a.b.seqs ? x.a.b.seqs[at] : at;
   // whether the group has more rows than `small` (the same answer for all of them)
   const int past = at + x.small / x.a.G;
-  s.tile = past < n && x.lead[past] == at;
+  s.kind = BLOCK;
+  if (TILES && past < n && x.lead[past] == at) s.kind = TILE;
+  else if (TILES && (int64_t)s.prefix * x.a.Hkv >= SIDE_BY_SIDE) s.kind = TWO_BLOCKS;
   ok = ok && s.prefix >= 0 && s.prefix <= x.max_prefix && s.seq >= 0 && s.seq < x.a.b.S;
   if (!ok && err && i0 + lane < n) atomicOr(err, NP_DEVERR_STATE);
   const bool alone = L == i && (i + 1 >= n || after != L);
@@ -115,9 +130,6 @@ __device__ inline int own_tid() {
 
 __device__ inline int lane_max(int v) { return (int)wave_max((uint32_t)(v + 1)) - 1; }  // v >= -1
 
-// Rows of the batch in a block of shared keys.
-__device__ inline int block_rows(bool tile, int G) { return (tile ? TB : RB) / G; }
-
 template <class T, int DP, bool FULL, bool E8>
 __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(SharedArgs x) {
   constexpr bool TILES = T::V == 8;
@@ -134,7 +146,7 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
   // of the rows i0 .. i0 + 63 (each wave finds the same): what would stand in the
   // way of the tiles' registers
   __shared__ struct {
-    int steps[WAVE], up_at[WAVE], lead[WAVE], name[WAVE], prefix[WAVE], lead_seq[WAVE], tile[WAVE];
+    int steps[WAVE], up_at[WAVE], lead[WAVE], name[WAVE], prefix[WAVE], lead_seq[WAVE], kind[WAVE];
     int groups[WAVE], us_at[WAVE], p0[WAVE], seq[WAVE];
   } rows;
   RowsLds& rl = *(RowsLds*)lds;
@@ -151,14 +163,13 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
   SharedRow sr;
   int steps, groups, up, us, up_at, us_at;
   auto load = [&](int first, int run_before, int32_t* e) {
-    sr = shared_row(x, first, run_before, e);
+    sr = shared_row<TILES>(x, first, run_before, e);
     const bool here = first + lane < n;
-    if (!TILES) sr.tile = false;
-    steps = sr.lead >= 0 && here && (first + lane - sr.lead) % block_rows(sr.tile, a.G) == 0
-                ? div_up_pos(sr.prefix, sr.tile ? TC::KB : GROUP)
+    steps = sr.lead >= 0 && here && (first + lane - sr.lead) % (kind_rows(sr.kind) / a.G) == 0
+                ? div_up_pos(sr.prefix, sr.kind == TILE ? TC::KB : GROUP)
                 : 0;
     groups = own_groups<KS>(sr.row.p0, sr.prefix, a.window);
-    up = steps ? x.cost(sr.tile).block(steps) * a.Hkv : 0;
+    up = steps ? x.cost(sr.kind == TILE).block(steps) * a.Hkv : 0;
     us = here ? x.own.block(groups) * nb : 0;
     up_at = (int)wave_incl_scan((uint32_t)up);
     us_at = (int)wave_incl_scan((uint32_t)us);
@@ -170,7 +181,7 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
     run = last(sr.run);
     tp += last(up_at);
     ts += last(us_at);
-    if (err && i + lane < n) x.row_lead[i + lane] = sr.lead < 0 ? -1 : sr.lead * 2 + sr.tile;
+    if (err && i + lane < n) x.row_lead[i + lane] = sr.lead < 0 ? -1 : sr.lead * 4 + sr.kind;
   }
   tp = uniform(tp);
   const int total = tp + uniform(ts);
@@ -202,8 +213,9 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
     // [kbeg, kend) that count
     int rho0 = 0, nrow, seq, h, minpos, maxpos, kbeg, kend, k0, k1;
     if (shared) {
-      const bool tile = uniform(rows.tile[at]);
-      const int RT = block_rows(tile, a.G), L = uniform(rows.lead[at]);
+      const int kind = uniform(rows.kind[at]);
+      const bool tile = kind == TILE;
+      const int RT = kind_rows(kind) / a.G, L = uniform(rows.lead[at]);
       seq = uniform(rows.lead_seq[at]);
       h = j;
       // its rows (up to RT of one group), and the positions they span
@@ -272,28 +284,41 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
       k0 = kbeg / KS * KS + c0 * GROUP;
       k1 = kbeg < kend ? min(kend, kbeg / KS * KS + c1 * GROUP) : k0;  // none: no step
     }
-    const int rho = rho0 + min(lane & 15, nrow - 1), b = b0 + rho / a.G, hq = h * a.G + rho % a.G;
-    const int p0 = row_p0(b);
-    f32x4 o[C::VS][C::NV];
-    float m, l;
-    bool missing;
-    rows_keys<T, DP, FULL, E8, true>(tid, a, a.table + (int64_t)seq * a.M, h, minpos, maxpos, kbeg,
-                                     kend, k0, k1,
-                                     a.q + (int64_t)b * a.q_stride + (int64_t)hq * a.D * W,
-                                     p0 < 0 ? maxpos : p0, o, m, l, missing);
-    if (missing && lane == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
-    rows_meet<C>(o, m, l, rl.o, rl.m, rl.l);
-    __syncthreads();
-    for (int u = tid; u < nrow * (DP / 4); u += ROWS_T) {
-      const int q = u / (DP / 4), d = u % (DP / 4) * 4;
-      float M, L;
-      const float4 sum = rows_met<C>(rl.o, rl.m, rl.l, q, d, M, L);
-      const int row = part_of(c0 == 0, shared ? 0 : n * x.Hq, b0 + (rho0 + q) / a.G,
-                              h * a.G + (rho0 + q) % a.G, q);
-      put(row, d, sum);
-      if (d == 0) *(float2*)(a.ml + (size_t)row * 2) = make_float2(M, L);
-    }
-    __syncthreads();  // LDS is free again
+    auto rows_part = [&](auto blocks) __attribute__((always_inline)) {
+      constexpr int QT = decltype(blocks)::value;
+      const char* qp[QT];
+      int qpos[QT];
+#pragma unroll
+      for (int i = 0; i < QT; ++i) {
+        const int rho = rho0 + min(RB * i + (lane & 15), nrow - 1);
+        const int b = b0 + rho / a.G, hq = h * a.G + rho % a.G, p0 = row_p0(b);
+        qp[i] = a.q + (int64_t)b * a.q_stride + (int64_t)hq * a.D * W;
+        qpos[i] = p0 < 0 ? maxpos : p0;
+      }
+      f32x4 o[QT][C::VS][C::NV];
+      float m[QT], l[QT];
+      bool missing;
+      rows_keys<T, DP, FULL, E8, true, QT>(tid, a, a.table + (int64_t)seq * a.M, h, minpos, maxpos,
+                                           kbeg, kend, k0, k1, qp, qpos, o, m, l, missing);
+      if (missing && lane == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
+#pragma unroll
+      for (int i = 0; i < QT; ++i) {
+        rows_meet<C>(o[i], m[i], l[i], rl.o, rl.m, rl.l);
+        __syncthreads();
+        for (int u = tid; u < min(RB, nrow - RB * i) * (DP / 4); u += ROWS_T) {
+          const int q = u / (DP / 4), d = u % (DP / 4) * 4, rho = rho0 + RB * i + q;
+          float M, L;
+          const float4 sum = rows_met<C>(rl.o, rl.m, rl.l, q, d, M, L);
+          const int row = part_of(c0 == 0, shared ? 0 : n * x.Hq, b0 + rho / a.G,
+                                  h * a.G + rho % a.G, RB * i + q);
+          put(row, d, sum);
+          if (d == 0) *(float2*)(a.ml + (size_t)row * 2) = make_float2(M, L);
+        }
+        __syncthreads();  // LDS is free again
+      }
+    };
+    if (TILES && nrow > RB) rows_part(std::integral_constant<int, TILES ? 2 : 1>{});
+    else rows_part(std::integral_constant<int, 1>{});
   };
 
   int pb = 0, sb = tp;  // weights before the chunk
@@ -311,7 +336,7 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
       rows.name[lane] = sr.name;
       rows.prefix[lane] = sr.prefix;
       rows.lead_seq[lane] = sr.seq;
-      rows.tile[lane] = sr.tile;
+      rows.kind[lane] = sr.kind;
       rows.groups[lane] = groups;
       rows.us_at[lane] = sb + us_at - us;
       rows.p0[lane] = sr.row.p0;
@@ -329,7 +354,7 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
         const int at = __ffsll((unsigned long long)hit) - 1;
         hit &= hit - 1;
         // this row's blocks that have units in the stretch
-        const Cost c = x.cost(shared && uniform(rows.tile[at]));
+        const Cost c = x.cost(shared && uniform(rows.kind[at]) == TILE);
         const int units = uniform(shared ? rows.steps[at] : rows.groups[at]);
         const int start = uniform(shared ? rows.up_at[at] : rows.us_at[at]);
         const int count = shared ? a.Hkv : nb, len = c.block(units);
@@ -358,8 +383,8 @@ __global__ __launch_bounds__(ROWS_T) void attn_shared_join_kernel(SharedArgs x) 
   if (id >= x.n * x.Hq) return;
   const int b = id / x.Hq, hq = id % x.Hq, h = hq / a.G, g = hq % a.G;
   const int per = (a.G + RB - 1) / RB, nb = per * a.Hkv;
-  const int named = load_scalar(x.row_lead, b), L = named >> 1;
-  const int RT = block_rows(named & 1, a.G);
+  const int named = load_scalar(x.row_lead, b), L = named >> 2;
+  const int RT = kind_rows(named & 3) / a.G;
   const int is = load_scalar(x.info_s, b * nb + g / RB * a.Hkv + h);
   const int b0 = L < 0 ? b : L + (b - L) / RT * RT;
   const int ip = L < 0 ? 0 : load_scalar(x.info_p, b0 * a.Hkv + h);

@@ -190,6 +190,21 @@ def test_long_prefix_is_split_and_joined(cache, dtype):
     assert torch.equal(a, s.run())
 
 
+@pytest.mark.parametrize("cache", ["same", "e4m3"])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,p,Hq,Hkv,D,P,window", [
+    (6, 20001, 16, 4, 64, 64, 0), (8, 20001, 16, 4, 64, 64, 19000), (11, 4200, 32, 16, 80, 16, 0),
+    (5, 17000, 16, 4, 128, 32, 0), (3, 8200, 64, 8, 256, 128, 0)])
+def test_two_row_blocks_side_by_side(cache, dtype, rows, p, Hq, Hkv, D, P, window):
+    """Up to 32 query heads per key-value head behind long prefixes, the second row block partly filled."""
+    if dtype == "f32" and D > 128:
+        pytest.skip("fp32 has no blocks side by side")
+    s = Setup([(p, [1 + 37 * i for i in range(rows)])], Hq, Hkv, D, P, dtype, cache, seed=rows)
+    out = s.run(window=window)
+    s.check(out, window=window, rows=[0, 1, rows - 1])
+    assert torch.equal(out, s.run(window=window)) and s.error() == 0
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_agrees_with_decode(dtype):
     """Without groups, and with every row a group of its own, within twice the bound of each."""

@@ -247,8 +247,8 @@ np_status np_kv_append(const np_kv_shape* shape, int32_t layer, const np_kv_batc
                        const np_rotary* rotary, void* pool, void* dev_ws, hipStream_t stream);
 
 /* The same behind a norm of each query and key head (norm NULL: none), all in
- * 32 bits up to the one rounding to w.  q_out, strides and what is not served as
- * above.  One kernel. */
+ * 32 bits up to the one rounding to w (keys of 8-bit caches in 64).  q_out,
+ * strides and what is not served as above.  One kernel. */
 np_status np_kv_append_norm(const np_kv_shape* shape, int32_t layer, const np_kv_batch* batch,
                             const int32_t* page_table, const np_kv_rows* rows,
                             const np_qk_norm* norm, const np_rotary* rotary, void* pool,

@@ -169,19 +169,18 @@ def test_norm_far_sizes():
     (5, 5, 16, 32, 0, False), (40, 8, 128, 128, 128, False), (2, 1, 256, 16, 256, True)])
 @pytest.mark.parametrize("eps", [None, 1e-5])
 def test_elements_bit_for_bit(dtype, Hq, Hkv, D, P, R, inter, eps):
-    """Keys that are the queries' heads too: the cache holds the elements of what q_out holds in w."""
+    """The cache holds the elements of the exact keys, rounded to w, and of the values."""
     s = Setup(ROWS, Hq, Hkv, D, P, dtype, "e4m3", seed=4)
-    s.qkv[:, Hq:Hq + Hkv] = s.qkv[:, :Hkv]
-    s.dev.copy_(s.qkv)
-    s.wk = s.wq
     cos, sin = rotary_tables(R, 200) if R else (None, None)
     s.append(eps, rotary=B.make_rotary(cos, sin, inter) if R else None)
     at = s.pos >= 0
     c, n = (cos.cpu(), sin.cpu()) if R else (None, None)
-    check(s, s.q_out.cpu()[at], s.qkv[:, :Hq], s.wq, eps, c, n, inter)
+    q, k, v = (x.cpu() for x in s.heads())
+    check(s, s.q_out.cpu()[at], q, s.wq, eps, c, n, inter)
+    keys, _ = norm_rotate(k[at], s.wk, eps, c, n, s.pos[at], inter, dtype)
     back = s.read()
-    for x, (byte, scale), r in zip((s.q_out[:, :Hkv], s.heads()[2]), s.stored(), back):
-        eb, es, ev = quantise(x.cpu()[at].double(), dtype)
+    for x, (byte, scale), r in zip((keys.float().to(DT[dtype]), v[at]), s.stored(), back):
+        eb, es, ev = quantise(x.double(), dtype)
         assert torch.equal(scale, es) and torch.equal(byte, eb)
         assert torch.equal(r[at].double(), ev) and torch.equal(values_of(byte, scale), ev)
         assert (r[~at] == 0).all()

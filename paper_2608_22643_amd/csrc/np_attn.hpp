@@ -249,7 +249,9 @@ __device__ inline float sum_groups(float v) {
 // are bound by the chain table -> keys -> scores -> values -> join: 8.9 us for
 // 777 keys and 32 heads.  fp32 prompts run here too: 4096 tokens of 16 heads over
 // 4 at 81, 74 and 93 TFLOP/s for heads of 64, 128 and 256 (an 8192^3 fp32 library
-// product reaches 149 to 154).
+// product reaches 149 to 154).  8-bit elements become w on their way to the matrix
+// cores: one row of 131071 keys, 8 key-value heads of 128, 270 MB in 47 us (5.7 TB/s);
+// 777 keys and 32 heads 8.8 us.
 // ---------------------------------------------------------------------------
 constexpr int RB = 16;
 constexpr int NWAVE = 4;
@@ -630,6 +632,8 @@ __device__ __forceinline__ float4 rows_met(const float (&s_o)[NWAVE][RB][C::OP],
 
 // EVEN: one token a row, the keys of all rows dealt evenly to the workgroups;
 // otherwise a workgroup per (block, head, split).
+// Workgroups a compute unit: 8-bit elements in flight take half the registers (64
+// rows of 47,000 keys in all, 8 key-value heads of 256: 62 us with one, 44 with two).
 template <class T, int DP, bool FULL, bool EVEN, bool E8>
 __global__ __launch_bounds__(ROWS_T, DP < 256 ? (E8 ? 3 : 2) : E8 ? 2 : 1) void attn_rows_kernel(
     AttnArgs a) {
@@ -920,6 +924,10 @@ __global__ __launch_bounds__(ROWS_T, DP < 256 ? (E8 ? 3 : 2) : E8 ? 2 : 1) void 
 // 980 TFLOP/s (an 8192^3 library product reaches 1140 to 1400, from card to card);
 // 2048 fp16 tokens and 32 heads 62 to 65 us (530 to 550 TFLOP/s; a library product
 // of as many operations 52 to 57 us).
+// 8-bit elements become w between registers and LDS; the second product reads as
+// before, at the same rates (8192 bf16 tokens of 64 heads over 8 of 128: 1.12 ms, 984
+// TFLOP/s).  Two stores a row meet in half of the banks; in an order of theirs that
+// does not it takes as long.
 // Measured and dropped: one workgroup of eight waves in two groups half a step
 // apart, 4.68 to 5.05 ms; the next step's score products dealt between this step's
 // exponentials, 4.56 ms (16384 tokens) and 119 against 106 us (packed prompts).
@@ -968,14 +976,15 @@ struct TileCfg {
 //
 // One stretch of keys [kbeg, kend) of the sequence with page table trow, K's head
 // h, against a tile's rows: this lane's query at qp has position qpos, those of its
-// wave lie in [wmin, wmax].  Afterwards a lane has its query's maximum m, half of its sum l
-// (the other half is lane ^ 32's) and its outputs o; missing: a key had no page.
+// wave lie in [wmin, wmax].  Afterwards a lane has its query's maximum m, half of
+// its sum l (the other half is lane ^ 32's) and its outputs o; missing: a key had no
+// page.
 // CUT: the rows may see keys from kend on, which other stretches have.
 template <class T, int DP, bool FULL, bool E8, bool CUT, class C = TileCfg<DP, E8>>
 __device__ __forceinline__ void tile_keys(int tid, const AttnArgs& a, const int32_t* trow, int h,
-                                          int kbeg, int kend, int wmin, int wmax, const char* qp, int qpos,
-                                          char* s_k, char* s_v, f32x16 (&o)[C::DT], float& m,
-                                          float& l, bool& missing) {
+                                          int kbeg, int kend, int wmin, int wmax, const char* qp,
+                                          int qpos, char* s_k, char* s_v, f32x16 (&o)[C::DT],
+                                          float& m, float& l, bool& missing) {
   constexpr int KB = C::KB, NL = C::NL, RSTEP = C::RSTEP, KT = C::KT, KD = DP / 16, DT = C::DT;
   const int lane = tid % WAVE;
   const int wave = uniform(tid / WAVE);
@@ -1295,8 +1304,8 @@ __global__ __launch_bounds__(TILE_T, DP == 256 ? 1 : 2) void attn_tile_kernel(At
   f32x16 o[DT];
   float m, l;
   bool missing;
-  tile_keys<T, DP, FULL, E8, false>(tid, a, a.table + (size_t)t.row.seq * a.M, h, kbeg, kend, wmin, wmax, qp,
-                             qpos, s_k, s_v, o, m, l, missing);
+  tile_keys<T, DP, FULL, E8, false>(tid, a, a.table + (size_t)t.row.seq * a.M, h, kbeg, kend, wmin,
+                                    wmax, qp, qpos, s_k, s_v, o, m, l, missing);
   if (missing && lane == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
 
   l = swap32_add(l, l);
@@ -1426,7 +1435,9 @@ hipError_t launch_tile(AttnArgs a, hipStream_t stream) {
 //  - More keys, several rows, whose lengths the host does not know: an even
 //    share of all keys to each of 512 workgroups (64 rows of 1 to 8192 keys:
 //    70, against 80 with the best fixed split of each row, most of whose
-//    workgroups find nothing to do).
+//    workgroups find nothing to do).  8-bit elements leave registers for three
+//    workgroups a compute unit up to heads of 128: 768 of them (64 rows of 47,000
+//    keys in all, 8 key-value heads, 97 MB: 27.1, with 512 30.4).
 // Prompts (rows of more tokens) have many blocks; they are split while those do
 // not give every compute unit two workgroups (64 tokens of 32 heads over 8 behind
 // 2000 others: 29 with one a compute unit, 23 with two), or one if they are few

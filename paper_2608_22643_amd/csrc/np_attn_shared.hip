@@ -9,6 +9,13 @@
 // 128 of them.  Small groups, all of fp32, and each row's own keys are row blocks
 // as in np_attn_decode: 16 query heads against keys in registers.
 //
+// What it costs beside the keys: the groups' search (2 us), a first step (5 to 7) and
+// the join (4 to 9).  32 fp16 rows of 32 heads over 8 of 128 in four groups behind up to 3000
+// keys take 22 us (np_attn_decode 35, of which the reads are 6.5): latencies in line.  48 bf16 rows
+// of 64 heads over 8 behind 32768 keys of 8-bit elements take 80 to 87 us (np_attn_decode 430,
+// the products alone 37 at the rate of a large one): 27 steps of a tile in each workgroup at
+// 2.2 to 2.9 us, and 33 MB of parts written and read.
+//
 // One kernel computes the parts, a second joins them.  The parts' keys lie on
 // a line (the tiles' first), weighed by what they cost, and every workgroup
 // has an equal stretch of it, whatever the lengths, which only the device
@@ -479,6 +486,11 @@ hipError_t launch_attn_shared(const np_kv_shape& s, int layer, const np_kv_batch
   const int64_t n = b.n_seq, heads = n * s.heads;
   SharedArgs x;
   x.a = attn_args(s, layer, b, table, q, q_stride, pool, scale, window, out, out_stride, ws);
+  auto apart = [&] {
+    return launch_attn(s, layer, b, table, q, q_stride, pool, scale, window, out, out_stride, ws,
+                       stream);
+  };
+  if (heads > KV_SHARED_HEADS || G > (dtype == NP_F32 ? RB : TB)) return apart();
   // The line counts 32 keys of a tile's rows: a row block's 128 keys cost as much as
   // a tile's 128 (its rows are fewer, but so are the keys in flight), and a tile's
   // beginning and end as much as four to eight of its steps.  Us with tiles' beginning
@@ -500,10 +512,7 @@ hipError_t launch_attn_shared(const np_kv_shape& s, int layer, const np_kv_batch
   // MB); 8 rows behind 512 9 / 15 (15 MB), behind 2048 18 / 16 (59 MB); 32 rows behind
   // 512 18 / 20 (65 MB), behind 2048 33 / 23 (260 MB).
   const int64_t saved = (n - 1) * sh.max_prefix * s.kv_heads * 2 * kv_row_bytes(s);
-  if (saved < (32 + n) * 1000000 || heads > KV_SHARED_HEADS ||
-      G > (dtype == NP_F32 ? RB : TB) || line >= ((int64_t)1 << 30))
-    return launch_attn(s, layer, b, table, q, q_stride, pool, scale, window, out, out_stride, ws,
-                       stream);
+  if (saved < (32 + n) * 1000000 || line >= ((int64_t)1 << 30)) return apart();
   KvScratch k;
   kv_ws_layout(s, (char*)ws, &k);
   x.lead = sh.lead;

@@ -733,11 +733,17 @@ __device__ inline uint4 round_row(const float* f) {
 // 2^lanes neighbouring lanes, so that its sum of squares and its largest magnitude
 // are reductions between lanes' registers.  A lane has NP pieces of 16 bytes: one
 // (rotary pairs that are neighbours, or none), or the two that turn into each
-// other (pairs i, i + R/2; behind the rotary part one).  A set is as many heads of
-// a token as a wave holds, all queries, all keys or all values, so that what a
-// wave does with them, and their addresses, are the same for its lanes.  The heads are
-// asked for before the token's place is looked up, and a set's before the one
-// before it is worked on: their addresses need only the token's number.
+// other (pairs i, i + R/2; behind the rotary part one; with one piece a lane, and
+// the partner's fetched from its lane, 124 us where this took 117).  A set is as
+// many heads of a token as a wave holds, all queries, all keys or all values, so
+// that what a wave does with them, and their addresses, are the same for its
+// lanes.  The heads are asked for before the token's place is looked up, and a
+// set's before the one before it is worked on: their addresses need only the
+// token's number.
+//
+// Bound by memory: 11,649 bf16 tokens, 64 + 8 + 8 heads of 128, normed, 483 MB in
+// 97 us (5.0 TB/s; a large copy reaches 5.1).  A few tokens take 4.0 to 4.8 us, a
+// chain of latencies.
 template <class T, int NP, bool E8>
 __global__ __launch_bounds__(APP_T) void kv_append_heads_kernel(AppendArgs a) {
   constexpr int V = T::V;
@@ -819,10 +825,11 @@ __global__ __launch_bounds__(APP_T) void kv_append_heads_kernel(AppendArgs a) {
   for (; set < sets; set += APP_T / WAVE) {
     Heads d = next;
     if (set + APP_T / WAVE < sets) next = load(set + APP_T / WAVE);
-    // A key next to the border of two elements, a sixteenth of it apart, goes where
-    // its exact value does: keys that become elements are normed and turned in 64
-    // bits (in 32, about 20 of 16.8 million fell to the other side; 4,113 tokens of
-    // 96 fp16 heads of 128 take 38 us, in 32 bits 32).
+    // Two elements are a sixteenth of their value apart, so that an error of 32 bits
+    // next to the border between them would grow to that: keys that become elements
+    // are normed and turned in 64 bits (in 32, about 20 of 16.8 million fell to the
+    // other side, in 64 none).  That costs a sixth: 38 us against 32 for 4106
+    // tokens of 32 fp16 heads over 32 of 128.
     bool done = false;
     if constexpr (E8) {
       if (d.kind == 1 && (a.norm || a.R)) {
@@ -974,7 +981,9 @@ __global__ __launch_bounds__(APP_T) void kv_append_heads_kernel(AppendArgs a) {
 
 // ---------------------------------------------------------------------------
 // np_kv_read: pieces of 16 bytes of a token's keys and values, NB of them a
-// thread, all asked for before the first is stored.
+// thread, all asked for before the first is stored.  Bound by memory, mostly of what
+// is written: 4,106 tokens of 32 heads of 128 from 8-bit elements to fp16, 101 MB in
+// 21.5 us (4.7 TB/s); a few tokens 3.2 us.
 // ---------------------------------------------------------------------------
 struct ReadArgs {
   KvBatch b;
@@ -1189,6 +1198,9 @@ hipError_t launch_kv_append(const np_kv_shape& s, int layer, const np_kv_batch& 
   const int per = WAVE >> a.lanes;
   a.sets = (s.heads + per - 1) / per + 2 * ((s.kv_heads + per - 1) / per);
   const int groups = (a.sets + APP_T / WAVE - 1) / (APP_T / WAVE);
+  // Few tokens: a workgroup for every four of a token's sets, while all of them are on the
+  // card at once (us, whole tokens / split: 17 tokens of 56 heads 6.7 / 4.6, 4097 tokens of 96
+  // heads 31.6 / 64).
   a.split = (int64_t)b.n_tokens * groups <= 2048;
   auto go = [&](auto kernel, int64_t blocks) {
     hipLaunchKernelGGL(kernel, block_grid(blocks), dim3(APP_T), 0, stream, a);
@@ -1229,6 +1241,8 @@ hipError_t launch_kv_read(const np_kv_shape& s, int layer, const np_kv_batch& b,
   a.M = s.seq_pages;
   a.N = s.n_pages;
   const int pieces = 2 * s.kv_heads * (s.head_dim / vec_elems(dtype));
+  // many pieces: four a thread, which find their token once (28.9 -> 21.5 us for the above);
+  // with few of them the workgroups count for more
   const bool many = pieces > 2 * APP_T && (int64_t)b.n_tokens * pieces > 2048 * APP_T;
   a.parts = (pieces + APP_T * (many ? 4 : 1) - 1) / (APP_T * (many ? 4 : 1));
   a.err = (int32_t*)((char*)ws + WS_ERR);

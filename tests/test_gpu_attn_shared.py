@@ -360,3 +360,33 @@ def test_graph_replays(cache):
         torch.cuda.synchronize()
         assert torch.equal(got, out)
     assert s.error() == 0
+
+
+def test_shapes_and_graphs_in_turn_on_one_workspace():
+    """Shared calls of three shapes and caches, eager and captured, in turn over one workspace: each gives the bits it
+    gives with a workspace of its own."""
+    runs = [Setup([(3000, [40, 9, 30, 1]), (700, [20, 9])], 8, 2, 128, 16, "bf16", "e4m3", seed=23),
+            Setup([(130, [1] * 70)], 32, 8, 64, 64, "f16", "same", seed=24),
+            Setup([(500, [7, "none", 3])], 4, 4, 80, 32, "f32", "same", seed=25)]
+    alone = [s.run() for s in runs]
+    for s, out in zip(runs, alone):
+        s.check(out)
+    ws = torch.zeros(max(s.ws.numel() for s in runs), dtype=torch.uint8, device=DEV)
+    graphs = []
+    for s in runs:
+        s.ws = ws
+        out, table, batch, shared = torch.zeros_like(s.qd), s.table.to(DEV), s.batch(), s.shared()
+        side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            B.np_attn_decode_shared(s.shape, 0, batch, shared, table, s.qd, s.pool, s.scale, 0, out, ws, side)
+        graphs.append((graph, out, table, batch, shared))
+    for turn in range(3):
+        for (graph, out, *_), s, want in zip(graphs, runs, alone):
+            out.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out.cpu(), want)
+            for other, w in zip(runs, alone):
+                assert torch.equal(other.run(), w)
+    assert B.np_device_error(ws) == 0

@@ -361,3 +361,57 @@ def test_graph_replays(cache):
         torch.cuda.synchronize()
         for a, b in zip(got, (s.q_out, s.pool, ko, vo)):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_past_4_gib(dtype):
+    """Elements, scales and read tokens beyond 4 GiB of a layer, in the second layer: the bytes of a small pool."""
+    s = Setup([(250, 20), (0, 30)], 8, 8, 128, 256, dtype, "e4m3", seed=12)
+    rot = B.make_rotary(*rotary_tables(128, 300))
+    s.append(1e-6, rotary=rot)
+    small, want = s.pool, s.read()
+    q_out, n = s.q_out.clone(), s.N
+    pages = (1 << 32) // (2 * 8 * 256 * 129) + 50
+    s.shape = B.make_kv_shape(2, 8, 8, 128, 256, pages, len(s.rows), s.M, dtype, "e4m3")
+    s.pool = torch.full(B.kv_pool_shape(s.shape), 111, dtype=torch.uint8, device=DEV)
+    s.ws = torch.zeros(B.np_kv_workspace_size(s.shape), dtype=torch.uint8, device=DEV)
+    s.tab = torch.where(s.tab >= 0, s.tab + pages - n, s.tab)
+    s.q_out.fill_(5)
+    s.append(1e-6, rotary=rot, layer=1)
+    assert torch.equal(s.pool[1, pages - n:], small[0]) and torch.equal(s.q_out, q_out)
+    assert (s.pool[1, :pages - n] == 111).all() and (s.pool[0] == 111).all()
+    assert all(torch.equal(x, y) for x, y in zip(s.read(1), want))
+    assert B.np_device_error(s.ws) == 0
+
+
+@pytest.mark.parametrize("cache", ["same", "e4m3"])
+def test_the_largest_batches(cache):
+    """A token in each of 4096 rows; 2^24 tokens, more than a launch has workgroups of 256 threads along an axis."""
+    s = Setup([(b % 7, 1) for b in range(4096)], 2, 1, 16, 16, "f16", cache, seed=13)
+    s.append(0.0, weights=False)
+    k, v = s.read()
+    x = s.qkv[:, 3:].double()
+    assert torch.equal(v.double(), quantise(x, "f16")[2] if cache == "e4m3" else x)
+    T = 1 << 24
+    dev = torch.zeros(T, 4, 16, dtype=torch.float16, device=DEV)
+    at = [0, 1, T // 2, T - 2, T - 1]
+    dev[at] = s.dev[:5]
+    # rows of two, one and two tokens, and the tokens between in rows that are not served
+    cu = i32([0, 2, T // 2, T // 2 + 1, T - 2, T])
+    pos0, seqs = i32([0, -1, 2, -1, 14]), i32([0, 3, 1, 3, 2])
+    batch = B.make_kv_batch(5, T, T, 16, pos0, seqs=seqs, cu_tokens=cu)
+    table = i32([[3], [1], [2], [0], [-1]])
+    shape = B.make_kv_shape(1, 2, 1, 16, 16, 4, 5, 1, "f16", cache)
+    pool = torch.zeros(B.kv_pool_shape(shape), dtype=s.pool.dtype, device=DEV)
+    ws = torch.zeros(B.np_kv_workspace_size(shape), dtype=torch.uint8, device=DEV)
+    q_out = torch.full((T, 2, 16), 5.0, dtype=torch.float16, device=DEV)
+    B.np_kv_append_norm(shape, 0, batch, table, B.make_qkv(dev[:, :2], dev[:, 2:3], dev[:, 3:], q_out),
+                        B.make_qk_norm(None, None, 0.0), None, pool, ws)
+    assert torch.equal(q_out[at], s.q_out[:5]) and (q_out[2:T // 2] == 5).all() and (q_out[T // 2 + 1:T - 2] == 5).all()
+    ko, vo = (torch.full((T, 1, 16), 9.0, dtype=torch.float16, device=DEV) for _ in range(2))
+    B.np_kv_read(shape, 0, batch, table, pool, ko, vo, ws)
+    assert torch.equal(ko[at].cpu(), k[:5]) and torch.equal(vo[at].cpu(), v[:5])
+    rest = torch.ones(T, dtype=torch.bool, device=DEV)
+    rest[at] = False
+    assert not ko[rest].any() and not vo[rest].any()  # tokens of rows that are not served
+    assert B.np_device_error(ws) == 0

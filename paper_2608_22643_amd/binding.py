@@ -424,6 +424,11 @@ def make_kv_shape(layers, heads, kv_heads, head_dim, page_size, n_pages, max_seq
                        DTYPE_CODE.get(dtype, dtype) | CACHE_CODE[cache])
 
 
+def _elem_size(dtype: int) -> int:
+    """Bytes of an element of the heads of np_kv_shape.dtype."""
+    return 4 if dtype & ~NP_KV_E4M3 == NP_F32 else 2
+
+
 def kv_pool_shape(shape: np_kv_shape) -> tuple[int, ...]:
     """Dimensions of a pool of np_kv_shape: of the type of the heads, or of bytes (e4m3)."""
     row = ((shape.page_size * (shape.head_dim + 1),) if shape.dtype & NP_KV_E4M3
@@ -473,8 +478,8 @@ def make_qk_norm(q_weight=None, k_weight=None, eps: float = 1e-6) -> np_qk_norm:
 def make_kv_shared(lead, prefix, max_prefix: int) -> np_kv_shared:
     """lead and prefix: int32 [n_seq] on the device, contiguous."""
     for x in (lead, prefix):
-        if hasattr(x, "is_contiguous") and not x.is_contiguous():
-            raise ValueError("lead and prefix: contiguous [n_seq] tensors")
+        if hasattr(x, "is_contiguous") and (not x.is_contiguous() or str(x.dtype) != "torch.int32"):
+            raise ValueError("lead and prefix: contiguous int32 [n_seq] tensors")
     return _kept(np_kv_shared(int(max_prefix), _p(lead), _p(prefix)), lead, prefix)
 
 
@@ -523,6 +528,10 @@ def np_kv_append(shape, layer: int, batch: np_kv_batch, page_table, rows: np_kv_
 
 def np_kv_append_norm(shape, layer: int, batch: np_kv_batch, page_table, rows: np_kv_rows, norm,
                       rotary, pool, ws, stream=None) -> None:
+    for w in getattr(norm, "_kept", ()):
+        if w is not None and (w.numel() != shape.head_dim
+                              or w.element_size() != _elem_size(shape.dtype)):
+            raise ValueError(f"weights: {shape.head_dim} values of the heads' type")
     _check(lib().np_kv_append_norm(ctypes.byref(shape), int(layer), ctypes.byref(batch),
                                    _p(page_table), ctypes.byref(rows),
                                    None if norm is None else ctypes.byref(norm),
@@ -533,6 +542,12 @@ def np_kv_append_norm(shape, layer: int, batch: np_kv_batch, page_table, rows: n
 def np_kv_read(shape, layer: int, batch: np_kv_batch, page_table, pool, k_out, v_out, ws,
                stream=None) -> None:
     """k_out and v_out: [tokens][kv_heads][head_dim] tensors, or None."""
+    for x in (k_out, v_out):
+        if x is not None and (tuple(x.shape[1:]) != (shape.kv_heads, shape.head_dim)
+                              or x.shape[0] < batch.n_tokens
+                              or x.element_size() != _elem_size(shape.dtype)):
+            raise ValueError(f"k_out and v_out: [{batch.n_tokens}][{shape.kv_heads}]"
+                             f"[{shape.head_dim}] tensors of the heads' type")
     ks, vs = (0 if x is None else _token_stride(x) for x in (k_out, v_out))
     _check(lib().np_kv_read(ctypes.byref(shape), int(layer), ctypes.byref(batch), _p(page_table),
                             _p(pool), _p(k_out), ks, _p(v_out), vs, _p(ws), _s(stream)),
@@ -560,6 +575,9 @@ def np_attn_prompt(shape, layer: int, batch: np_kv_batch, page_table, q, pool, s
 def np_attn_decode_shared(shape, layer: int, batch: np_kv_batch, shared: np_kv_shared, page_table, q,
                           pool, scale: float, window: int, out, ws, stream=None) -> None:
     """q and out: [tokens][heads][head_dim] tensors."""
+    for x in getattr(shared, "_kept", ()):
+        if hasattr(x, "numel") and x.numel() != batch.n_seq:
+            raise ValueError(f"lead and prefix have {x.numel()} rows, the batch {batch.n_seq}")
     _check(lib().np_attn_decode_shared(ctypes.byref(shape), int(layer), ctypes.byref(batch),
                                        ctypes.byref(shared), _p(page_table), _p(q),
                                        _token_stride(q), _p(pool), float(scale), int(window),

@@ -166,3 +166,30 @@ def test_norm_reference():
     assert torch.equal(normed(torch.zeros(1, 1, 8), None, 0.0), torch.zeros(1, 1, 8, dtype=torch.float64))
     w = torch.tensor([1.0, 2.0, 3.0, 4.0])
     assert torch.allclose(normed(x, w, 0.75), x.double() * w / math.sqrt(7.0))
+
+
+@pytest.mark.parametrize("cache", ["same", "e4m3"])
+def test_tensors_of_other_sizes_are_refused(cache):
+    """The binding knows what the pointers cannot tell: nothing is read or written past a tensor."""
+    s, b = shape(cache=cache), batch()
+    half, D, n = torch.float16, s.head_dim, b.n_tokens
+    norms = [B.make_qk_norm(torch.ones(D // 2, dtype=half)), B.make_qk_norm(None, torch.ones(2 * D, dtype=half)),
+             B.make_qk_norm(torch.ones(D))]
+    outs = [torch.zeros(n - 1, s.kv_heads, D, dtype=half), torch.zeros(n, s.kv_heads + 1, D, dtype=half),
+            torch.zeros(n, s.kv_heads, D // 2, dtype=half), torch.zeros(n, s.kv_heads, D)]
+    for norm in norms:
+        with pytest.raises(ValueError):
+            B.np_kv_append_norm(s, 0, b, 16, rows(), norm, None, 16, 16)
+    for x in outs:
+        for k, v in ((x, None), (None, x)):
+            with pytest.raises(ValueError):
+                B.np_kv_read(s, 0, b, 16, 16, k, v, 16)
+    i32 = torch.zeros(b.n_seq + 1, dtype=torch.int32)
+    q = torch.zeros(b.n_seq, s.heads, D, dtype=half)
+    with pytest.raises(ValueError):
+        B.np_attn_decode_shared(s, 0, b, B.make_kv_shared(i32, i32, 5), 16, q, 16, 1.0, 0, q, 16)
+    for x in (i32.long(), i32.float(), torch.zeros(8, dtype=torch.int32)[::2]):
+        with pytest.raises(ValueError):
+            B.make_kv_shared(x, i32, 5)
+        with pytest.raises(ValueError):
+            B.make_kv_shared(i32, x, 5)

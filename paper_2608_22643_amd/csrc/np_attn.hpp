@@ -287,12 +287,13 @@ struct RowsCfg {
 // One stretch of keys: the rows of a block against keys [k0, k1) of its [kbeg,
 // kend), K's head h, this lane's query at qp (position qpos), the pages of the
 // sequence with page table trow.  minpos and maxpos bound the rows' positions.
-// Each wave takes every fourth step, and has its own maximum m, sum l and
+// Each of NW waves takes every NW-th step, and has its own maximum m, sum l and
 // outputs o afterwards; missing: a key had no page.
 // CUT: the rows may see keys before kbeg or from kend on, which other stretches have.
 // QT: blocks of 16 rows at once, each with its own queries and results; the keys
 // and values are loaded, and turned into operands, for all of them together.
-template <class T, int DP, bool FULL, bool E8, bool CUT, int QT, class C = RowsCfg<T, DP, E8>>
+template <class T, int DP, bool FULL, bool E8, bool CUT, int QT, int NW = NWAVE,
+          class C = RowsCfg<T, DP, E8>>
 __device__ __forceinline__ void rows_keys(int tid, const AttnArgs& a, const int32_t* trow, int h,
                                           int minpos, int maxpos, int kbeg, int kend, int k0, int k1,
                                           const char* const (&qp)[QT], const int (&qpos)[QT],
@@ -301,7 +302,7 @@ __device__ __forceinline__ void rows_keys(int tid, const AttnArgs& a, const int3
   constexpr int V = C::V, W = C::W, KS = C::KS, KT = C::KT, KD = C::KD, KP = C::KP, NS = C::NS,
                 NV = C::NV, VS = C::VS, VR = C::VR;
   const int lane = tid % WAVE;
-  const int wave = uniform(tid / WAVE);
+  const int wave = NW == 1 ? 0 : uniform(tid / WAVE);
   const int r = lane & 15, g = lane >> 4;
   const int klast = max(kend - 1, 0);
   // the keys that this lane's query counts
@@ -441,7 +442,7 @@ __device__ __forceinline__ void rows_keys(int tid, const AttnArgs& a, const int3
   // one's are used, so that loads are in flight during all of the arithmetic.
   auto step = [&](auto last) {
     constexpr bool LAST = decltype(last)::value;
-    const int next = base + NWAVE * KS;
+    const int next = base + NW * KS;
     load_v();
     __builtin_amdgcn_sched_barrier(0);
     const bool full = ok == 3 && base + KS - 1 <= minpos &&
@@ -467,7 +468,7 @@ __device__ __forceinline__ void rows_keys(int tid, const AttnArgs& a, const int3
       // of their own
       __builtin_amdgcn_sched_barrier(0);
       load_k(next, pg);
-      pg = pages_of(next + NWAVE * KS);
+      pg = pages_of(next + NW * KS);
     }
     const bool has = (ok >> (KS == 32 && g >= 2 ? 1 : 0)) & 1;
     uint4 pb[QT];
@@ -572,10 +573,10 @@ __device__ __forceinline__ void rows_keys(int tid, const AttnArgs& a, const int3
     load_k(base, pg);
     ok = next_ok;
     missing |= ok != 3;
-    pg = pages_of(base + NWAVE * KS);
-    if (base + NWAVE * KS < k1) {
+    pg = pages_of(base + NW * KS);
+    if (base + NW * KS < k1) {
       do step(std::false_type{});
-      while (base + NWAVE * KS < k1);
+      while (base + NW * KS < k1);
     }
     step(std::true_type{});
   }
@@ -903,6 +904,56 @@ __global__ __launch_bounds__(ROWS_T, DP < 256 ? (E8 ? 3 : 2) : E8 ? 2 : 1) void 
       __syncthreads();  // LDS is free again
     }
   }
+}
+
+// One token a row, a wave for all keys of a block: no exchange between waves, and
+// as many blocks under way as the card holds waves.  A lane has its query's
+// outputs, NV of them together, so they leave from the registers.
+template <class T, int DP, bool FULL, bool E8>
+__global__ __launch_bounds__(ROWS_T, DP < 256 ? (E8 ? 3 : 2) : E8 ? 2 : 1) void attn_waves_kernel(
+    AttnArgs a) {
+  using C = RowsCfg<T, DP, E8>;
+  constexpr int V = C::V, W = C::W, NV = C::NV;
+  const int lane = threadIdx.x % WAVE, r = lane & 15, g = lane >> 4;
+  const int id = uniform(grid_block() * NWAVE + (int)threadIdx.x / WAVE);
+  const int per = (a.G + RB - 1) / RB, nb = per * a.Hkv;
+  const int row = id / nb, j = id % nb, h = j % a.Hkv;
+  if (row >= a.b.n_seq) return;
+  Tile t;
+  make_tile<RB>(kv_row(a.b, row, j == 0 && lane == 0 ? a.err : nullptr), a.G, j / a.Hkv, &t);
+  for (int* p : {&t.row.begin, &t.row.p0, &t.row.seq, &t.minpos, &t.maxpos}) *p = uniform(*p);
+  const int kbeg = first_key(t, a.window), kend = t.maxpos + 1;
+  const int head = h * a.G + t.rho0 + min(r, t.nrow - 1);
+  const char* const qp[1] = {a.q + (int64_t)t.row.begin * a.q_stride + (int64_t)head * a.D * W};
+  const int qpos[1] = {t.row.p0};
+  f32x4 o[1][C::VS][NV];
+  float m[1], l[1];
+  bool missing;
+  rows_keys<T, DP, FULL, E8, false, 1, 1>(threadIdx.x, a, a.table + (int64_t)t.row.seq * a.M, h,
+                                          t.minpos, t.maxpos, kbeg, kend, kbeg / C::KS * C::KS,
+                                          kend, qp, qpos, o, m, l, missing);
+  if (missing && lane == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
+  const float sum = sum_groups(l[0]), inv = 1.f / sum;
+  const bool none = sum == 0.f;  // a row that sees nothing is zero
+  if (r >= t.nrow) return;
+  char* op = a.out + (int64_t)t.row.begin * a.out_stride + (int64_t)head * a.D * W;
+#pragma unroll
+  for (int s = 0; s < C::VS; ++s)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int d = 16 * NV * s + NV * (4 * g + i);
+      if (d >= a.D) continue;
+      float f[NV];
+#pragma unroll
+      for (int x = 0; x < NV; ++x) f[x] = none ? 0.f : o[0][s][x][i] * inv;
+#pragma unroll
+      for (int x = 0; x < NV; x += 4)
+        if constexpr (V == 8)
+          *(uint2*)(op + (d + x) * W) = make_uint2(pack2<T>(f[x], f[x + 1]),
+                                                   pack2<T>(f[x + 2], f[x + 3]));
+        else
+          *(float4*)(op + (d + x) * W) = make_float4(f[x], f[x + 1], f[x + 2], f[x + 3]);
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -1424,7 +1475,7 @@ hipError_t launch_tile(AttnArgs a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// keys: the most a block can see.  Three ways to deal the keys of `blocks`
+// keys: the most a block can see.  Four ways to deal the keys of `blocks`
 // blocks to workgroups (us, fp16 or bf16, D 128, before -> with the rule):
 //  - Every 128 keys to a workgroup of its own while all of them fit on the card
 //    at once (three to a compute unit): one row of 777 keys and 32 heads 9.3
@@ -1438,6 +1489,14 @@ hipError_t launch_tile(AttnArgs a, hipStream_t stream) {
 //    workgroups find nothing to do).  8-bit elements leave registers for three
 //    workgroups a compute unit up to heads of 128: 768 of them (64 rows of 47,000
 //    keys in all, 8 key-value heads, 97 MB: 27.1, with 512 30.4).
+//  - Many blocks of few keys: each would cost its workgroup the whole chain from
+//    table to join for a step or two of its waves; up to 256 keys a wave has a
+//    block to itself, and all of them are under way at once.  Us, even shares / a
+//    wave each, rows of 1 to 64, 256 and 512 keys: 8-bit elements, 32 rows of 32
+//    heads over 32 11.1 / 6.1, 19.7 / 12.9, 22.2 / 21.3, 160 rows 30.8 / 13.5, 53.6 /
+//    36.5, 96.6 / 72.4; fp16 36.4 / 18.9, 87.8 / 75.0, 152 / 145; fp32 of 64 and 8-bit
+//    elements 34.3 / 17.2, 71 / 47, 109 / 95; but with 512 blocks, 64 rows of 32 over
+//    8, of 256 keys 12.6 / 11.6, 13.3 / 13.8, 14.6 / 19.6.
 // Prompts (rows of more tokens) have many blocks; they are split while those do
 // not give every compute unit two workgroups (64 tokens of 32 heads over 8 behind
 // 2000 others: 29 with one a compute unit, 23 with two), or one if they are few
@@ -1453,6 +1512,15 @@ hipError_t launch_rows(AttnArgs a, int64_t keys, int max_tokens, hipStream_t str
   // the line of groups is counted in 32 bits
   const bool even = !a.b.cu && !small && a.b.n_seq > 1 && groups * blocks < ((int64_t)1 << 30);
   dim3 grid;
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(ROWS_T), 0, stream, a);
+    return hipGetLastError();
+  };
+  if (!a.b.cu && !small && blocks > 768 && keys <= 256) {
+    grid = block_grid((blocks + NWAVE - 1) / NWAVE);
+    if (a.D == DP) return go(attn_waves_kernel<T, DP, true, E8>);
+    return go(attn_waves_kernel<T, DP, false, E8>);
+  }
   if (even) {
     a.chunk = (int)((groups + MAX_SPLITS - 3) / (MAX_SPLITS - 2));
     grid.x = E8 && DP <= 128 ? 768 : 512;
@@ -1468,10 +1536,6 @@ hipError_t launch_rows(AttnArgs a, int64_t keys, int max_tokens, hipStream_t str
     a.splits = (int)((keys + a.chunk - 1) / a.chunk);
     grid = block_grid(blocks * a.splits);
   }
-  auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(ROWS_T), 0, stream, a);
-    return hipGetLastError();
-  };
   if (even) {
     if (a.D == DP) return go(attn_rows_kernel<T, DP, true, true, E8>);
     return go(attn_rows_kernel<T, DP, false, true, E8>);

@@ -41,6 +41,8 @@ struct Cost {
   __device__ int place(int unit) const { return fix + unit * w; }
 };
 
+constexpr int SH_WG = 512;  // workgroups at most
+
 struct SharedArgs {
   AttnArgs a;
   const int32_t *lead, *prefix;
@@ -48,14 +50,18 @@ struct SharedArgs {
   int Hq, n;
   int least;  // weight of a stretch at least
   int small;  // most query heads per key-value head of a group that has row blocks
-  Cost tile, own;
+  int alone;  // groups of a row's own keys, at most, that a wave takes by itself
+  Cost tile, own, few;
   int32_t *info_p, *info_s, *row_lead;
   __device__ Cost cost(bool is_tile) const {
     return {is_tile ? tile.fix : own.fix, is_tile ? tile.w : own.w};
   }
+  // of a row's own keys
+  __device__ Cost cost_own(int groups) const {
+    return {groups <= alone ? few.fix : own.fix, groups <= alone ? few.w : own.w};
+  }
 };
 
-constexpr int SH_WG = 512;    // workgroups at most
 constexpr int FAR = 1 << 30;  // past all positions
 static_assert(2 * KV_SHARED_HEADS + SH_WG * TB <= KV_PART_ROWS, "rows of all parts fit");
 
@@ -177,7 +183,7 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
                 : 0;
     groups = own_groups<KS>(sr.row.p0, sr.prefix, a.window);
     up = steps ? x.cost(sr.kind == TILE).block(steps) * a.Hkv : 0;
-    us = here ? x.own.block(groups) * nb : 0;
+    us = here ? x.cost_own(groups).block(groups) * nb : 0;
     up_at = (int)wave_incl_scan((uint32_t)up);
     us_at = (int)wave_incl_scan((uint32_t)us);
   };
@@ -328,6 +334,37 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
     else rows_part(std::integral_constant<int, 1>{});
   };
 
+  // All of block j of row i0 + at's own keys, by this wave: no exchange with others.
+  auto wave_part = [&](int at, int j) __attribute__((always_inline)) {
+    const int lane = own_tid() % WAVE;
+    const int b = i0 + at, h = j % a.Hkv, rho0 = j / a.Hkv * RB, nrow = min(RB, a.G - rho0);
+    const int pos = uniform(rows.p0[at]), seq = uniform(rows.seq[at]);
+    const int kbeg = own_first<KS>(pos, uniform(rows.prefix[at]), a.window), kend = pos + 1;
+    const int k0 = kbeg / KS * KS, hq = h * a.G + rho0 + min(lane & 15, nrow - 1);
+    const char* const qp[1] = {a.q + (int64_t)b * a.q_stride + (int64_t)hq * a.D * W};
+    const int qpos[1] = {pos};
+    f32x4 o[1][C::VS][C::NV];
+    float m[1], l[1];
+    bool missing;
+    rows_keys<T, DP, FULL, E8, true, 1, 1>(lane, a, a.table + (int64_t)seq * a.M, h, pos, pos, kbeg,
+                                           kend, k0, kbeg < kend ? kend : k0, qp, qpos, o, m, l,
+                                           missing);
+    if (missing && lane == 0) atomicOr(a.err, NP_DEVERR_NOT_RESIDENT);
+    l[0] = sum_groups(l[0]);
+    if (lane == 0) x.info_s[b * nb + j] = wg | wg << 16;
+    if ((lane & 15) >= nrow) return;
+    const int g = lane >> 4, row = part_of(true, n * x.Hq, b, hq, 0);
+#pragma unroll
+    for (int s = 0; s < C::VS; ++s)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int y = 0; y < C::NV; y += 4)
+          put(row, 16 * C::NV * s + C::NV * (4 * g + i) + y,
+              make_float4(o[0][s][y][i], o[0][s][y + 1][i], o[0][s][y + 2][i], o[0][s][y + 3][i]));
+    if (g == 0) *(float2*)(a.ml + (size_t)row * 2) = make_float2(m[0], l[0]);
+  };
+
   int pb = 0, sb = tp;  // weights before the chunk
   run = 0;
   for (; i0 < n && (pb < min(tp, end) || sb < end); i0 += WAVE) {
@@ -361,8 +398,8 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
         const int at = __ffsll((unsigned long long)hit) - 1;
         hit &= hit - 1;
         // this row's blocks that have units in the stretch
-        const Cost c = x.cost(shared && uniform(rows.kind[at]) == TILE);
         const int units = uniform(shared ? rows.steps[at] : rows.groups[at]);
+        const Cost c = shared ? x.cost(uniform(rows.kind[at]) == TILE) : x.cost_own(units);
         const int start = uniform(shared ? rows.up_at[at] : rows.us_at[at]);
         const int count = shared ? a.Hkv : nb, len = c.block(units);
         int32_t* const info = shared ? x.info_p : x.info_s;
@@ -371,6 +408,16 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
           if (x0 >= end) break;
           const int c0 = min(units, c.unit(beg - x0)), c1 = min(units, c.unit(end - x0));
           if (c0 >= c1) continue;
+          if (!shared && units <= x.alone && c0 == 0 && c1 == units) {
+            // this block and the next ones that are here as a whole, a wave each
+            int many = 1;
+            while (many < NWAVE && j + many < count &&
+                   x0 + many * len + c.place(units - 1) < end)
+              ++many;
+            if (wave < many) wave_part(at, j + wave);
+            j += many - 1;
+            continue;
+          }
           if (c0 == 0 && threadIdx.x == 0)
             info[(i0 + at) * count + j] = wg | (x0 + c.place(units - 1)) / share << 16;
           part(shared, at, j, c0, c1);
@@ -499,6 +546,15 @@ hipError_t launch_attn_shared(const np_kv_shape& s, int layer, const np_kv_batch
   // 8-bit elements 79.7 / 87.6 / 104.9 / 86.1.
   x.tile = {8, s.head_dim > 128 ? 1 : 2};
   x.own = {0, 4};
+  // More blocks of own keys than workgroups, which would have them one after the other:
+  // up to 256 keys in a wave each, four of them in the time of two of the others.  Us, all
+  // waves on a block / a wave a block (weight 1): 90 fp16 rows of 40 heads over 40 in three
+  // groups behind up to 1500 keys, 1 to 60 of their own 51.5 / 39.6 (41.7), of 32 over 32
+  // behind 300 36.3 / 29.9 (28.0), of 40 over 8 behind 1500 31.3 / 28.2 (27.4); 20 of 32 over
+  // 32 of 256 behind 1000, 1 to 250 of their own 38.6 / 28.8 (36.5); but with 256 blocks, 32
+  // rows of 32 over 8 behind 3000, 1 to 300 of their own 22.3 / 24.6 (26.1).
+  x.few = {0, 2};
+  x.alone = heads / G * ((G + RB - 1) / RB) > SH_WG ? 2 : 0;
   x.least = 4;
   x.small = dtype == NP_F32 ? 0 : 32;
   // the line's length: at most a block of shared keys a row, and every row's own

@@ -390,3 +390,34 @@ def test_shapes_and_graphs_in_turn_on_one_workspace():
             for other, w in zip(runs, alone):
                 assert torch.equal(other.run(), w)
     assert B.np_device_error(ws) == 0
+
+
+@pytest.mark.parametrize("cache", ["same", "e4m3"])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("window", [0, 20, 150])
+@pytest.mark.parametrize("Hq,Hkv,D,P", [(16, 16, 64, 16), (32, 8, 128, 32), (40, 8, 80, 16), (16, 16, 256, 64),
+                                        (24, 24, 16, 16)])
+def test_many_rows_with_few_keys_of_their_own(cache, dtype, window, Hq, Hkv, D, P):
+    """More blocks of own keys than workgroups: a wave each, up to 256 keys; rows with more, with none and
+    not served, and inside the prefix, beside them."""
+    owns = [1, 16, 17, 33, 127, 128, 129, 255, 256, 257, 300, "none", 0, -3, 2, 60, 100, 7]
+    groups = [(90, owns * 2), (33, [5, "none", 9]), (0, owns[:7]), (17, [1] * 23)]
+    s = Setup(groups, Hq, Hkv, D, P, dtype, cache, seed=26)
+    assert s.n * Hkv > 512
+    out = s.run(window=window)
+    s.check(out, window=window, rows=range(30 if D > 128 else s.n))
+    assert s.error() == 0
+    assert torch.equal(out, s.run(window=window))
+
+
+def test_a_missing_page_of_own_keys_that_a_wave_has():
+    s = Setup([(70, [90, 30] + [40] * 40)], 16, 16, 64, 16, "bf16", seed=27)
+    clean = s.run()
+    table = s.table.clone()
+    table[0, 6] = -1  # positions 96 .. 111 of row 0
+    out = s.run(table=table.to(DEV))
+    assert s.error() == B.NP_DEVERR_NOT_RESIDENT
+    assert torch.equal(out[1:], clean[1:])
+    at = torch.cat((torch.arange(96), torch.arange(112, 160)))
+    ref, tol = attention(s.q[:1], s.keys[0][:, at], s.values[0][:, at], len(at) - 1, s.scale, 0, "bf16")
+    assert ((out[0].double() - ref[0]).abs() <= tol[0]).all()

@@ -568,7 +568,11 @@ hipError_t launch_attn_shared(const np_kv_shape& s, int layer, const np_kv_batch
   // MB); 8 rows behind 512 9 / 15 (15 MB), behind 2048 18 / 16 (59 MB); 32 rows behind
   // 512 18 / 20 (65 MB), behind 2048 33 / 23 (260 MB).
   const int64_t saved = (n - 1) * sh.max_prefix * s.kv_heads * 2 * kv_row_bytes(s);
-  if (saved < (32 + n) * 1000000 || line >= ((int64_t)1 << 30)) return apart();
+  // Rows of up to 256 keys of 8-bit elements, many blocks: np_attn_decode has a wave for each
+  // (36 rows of 40 heads over 40, 192 keys shared, 17.3 / 20.1; 160 of 32 over 32 34.2 / 37.5
+  // to 41.3; plain fp16 25.0 / 21.9, 50.0 / 47.9).
+  const bool brief = kv_e4m3(s) && x.a.b.lim <= 256 && (int64_t)x.a.tiles * s.kv_heads > 768;
+  if (saved < (32 + n) * 1000000 || brief || line >= ((int64_t)1 << 30)) return apart();
   KvScratch k;
   kv_ws_layout(s, (char*)ws, &k);
   x.lead = sh.lead;

@@ -154,7 +154,8 @@ typedef struct np_rotary {
 /* Norms of the query and key heads: q_weight and k_weight, device, type w, [D],
  * 16-byte aligned, each NULL for ones; a head x becomes
  *     x_d weight_d / sqrt(mean of x_d^2 over the head + eps)    (fp32).
- * eps: finite, >= 0.  (A head of zeros stays zero, also when eps is 0.) */
+ * eps: finite, >= 0.  (A head of zeros stays zero, also when eps is 0; one with a
+ * NaN becomes NaN.) */
 typedef struct np_qk_norm {
   const void* q_weight;
   const void* k_weight;

@@ -845,7 +845,7 @@ __global__ __launch_bounds__(APP_T) void kv_append_heads_kernel(AppendArgs a) {
 #pragma unroll
           for (int e = 0; e < NP * V; ++e) ss = __builtin_fma((double)f[e], (double)f[e], ss);
           const double mean = sum_lanes(ss, a.lanes) * a.inv_dim64 + (double)a.eps;
-          r = mean > 0.0 ? rsqrt64(mean) : 0.0;
+          r = mean == 0.0 ? 0.0 : rsqrt64(mean);  // of a NaN, NaN
         }
         const bool weighed = a.norm && a.wk;
         auto value = [&](int e) {
@@ -883,7 +883,7 @@ __global__ __launch_bounds__(APP_T) void kv_append_heads_kernel(AppendArgs a) {
         for (int p = 0; p < NP; ++p) ss = T::dot(d.x[p], d.x[p], ss);
         ss = reduce_lanes(ss, a.lanes, add);
         const float mean = ss * a.inv_dim + a.eps;
-        float r = mean > 0.f ? __builtin_amdgcn_rsqf(mean) : 0.f;
+        float r = mean == 0.f ? 0.f : __builtin_amdgcn_rsqf(mean);  // of a NaN, NaN
         const bool far = !(ss < 1e36f) || mean < 1e-27f;
         if (__any(d.live && far)) {
           float m = 0.f;

@@ -88,7 +88,7 @@ __device__ inline int kind_rows(int kind) {
 struct SharedRow {
   KvRow row;
   int lead;    // the first row of its group, or -1: by itself
-  int prefix;  // positions it has in common with it
+  int prefix;  // positions below max_len it has in common with it
   int seq;     // the lead's sequence
   int run;     // the first of the neighbouring rows that name the same lead
   int name;    // the lead that the row names
@@ -106,14 +106,17 @@ __device__ inline SharedRow shared_row(const SharedArgs& x, int i0, int run_befo
   s.run = cuts ? i0 + 63 - __clzll((long long)cuts) : run_before;
   bool ok = L >= 0 && L <= i && s.run <= L;
   const int at = ok ? L : 0;
-  s.prefix = x.prefix[at];
+  const int prefix = x.prefix[at];
+  // positions past max_len and the table are seen by no row, and sums with a prefix that
+  // has them would leave 32 bits
+  s.prefix = min(prefix, x.a.b.lim);
   s.seq = x.a.b.seqs ? x.a.b.seqs[at] : at;
   // whether the group has more rows than `small` (the same answer for all of them)
   const int past = at + x.small / x.a.G;
   s.kind = BLOCK;
   if (TILES && past < n && x.lead[past] == at) s.kind = TILE;
   else if (TILES && (int64_t)s.prefix * x.a.Hkv >= SIDE_BY_SIDE) s.kind = TWO_BLOCKS;
-  ok = ok && s.prefix >= 0 && s.prefix <= x.max_prefix && s.seq >= 0 && s.seq < x.a.b.S;
+  ok = ok && prefix >= 0 && prefix <= x.max_prefix && s.seq >= 0 && s.seq < x.a.b.S;
   if (!ok && err && i0 + lane < n) atomicOr(err, NP_DEVERR_STATE);
   const bool alone = L == i && (i + 1 >= n || after != L);
   s.lead = ok && !alone && s.prefix > 0 ? L : -1;
@@ -559,7 +562,8 @@ hipError_t launch_attn_shared(const np_kv_shape& s, int layer, const np_kv_batch
   x.small = dtype == NP_F32 ? 0 : 32;
   // the line's length: at most a block of shared keys a row, and every row's own
   const int64_t line =
-      n * s.kv_heads * (((int64_t)sh.max_prefix / 32 + 1) * x.tile.w + x.tile.fix + x.own.fix) +
+      n * s.kv_heads *
+          ((std::min<int64_t>(sh.max_prefix, x.a.b.lim) / 32 + 1) * x.tile.w + x.tile.fix + x.own.fix) +
       heads * (((int64_t)x.a.b.lim / GROUP + 2) * x.own.w + x.own.fix);
   // What sharing saves is at most the prefix's bytes for all rows but one; the join,
   // and the search for the groups, cost 4 us and 0.1 a row, about what 32 MB and 1

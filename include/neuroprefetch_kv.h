@@ -295,7 +295,7 @@ np_status np_attn_prompt(const np_kv_shape* shape, int32_t layer, const np_kv_ba
  * rounding of sums in another order; the same bits from run to run), but the
  * keys and values of a group's prefix are read once for its rows together, each
  * row's other keys after that.  Two kernels, the second to join the parts.  Where
- * little can be gained (max_prefix and the batch bound what sharing saves: up to
+ * little can be gained (max_prefix, window and batch bound what sharing saves: up to
  * some 30 MB of keys and values it is not worth the second kernel, nor for many short
  * rows of 8-bit elements), and for batches
  * of more than 32768 query heads in all, or more than 128 query heads per key-value

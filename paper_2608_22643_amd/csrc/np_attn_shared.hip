@@ -72,6 +72,14 @@ __device__ inline KvRow lane_row(const KvBatch& b, int i, int32_t* err) {
   return kv_row_check(b, {i, i + 1, b.seqs ? b.seqs[i] : i, b.pos0[i]}, err);
 }
 
+// The thread's number, anew for each part: what the parts derive from it would
+// otherwise be kept for all of them at once, past the registers there are.
+__device__ inline int own_tid() {
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  return tid;
+}
+
 // What a group's shared keys are computed in: row blocks, two of them side by side
 // (the keys loaded once for both), or tiles.  Two side by side pay where the keys are
 // bound by memory and not by one unit's latency (us, one block after the other / side
@@ -96,7 +104,7 @@ struct SharedRow {
 };
 template <bool TILES>
 __device__ inline SharedRow shared_row(const SharedArgs& x, int i0, int run_before, int32_t* err) {
-  const int lane = threadIdx.x % WAVE, n = x.n;
+  const int lane = own_tid() % WAVE, n = x.n;
   const int i = min(i0 + lane, n - 1);
   SharedRow s;
   const int L = x.lead[i], before = x.lead[max(i - 1, 0)], after = x.lead[min(i + 1, n - 1)];
@@ -136,15 +144,32 @@ __device__ inline int own_groups(int p0, int prefix, int window) {
   return max(1, div_up_pos(p0 + 1 - first, GROUP));
 }
 
-// The thread's number, anew for each part: what the parts derive from it would
-// otherwise be kept for all of them at once, past the registers there are.
-__device__ inline int own_tid() {
-  int tid = threadIdx.x;
-  asm volatile("" : "+v"(tid));
-  return tid;
-}
-
 __device__ inline int lane_max(int v) { return (int)wave_max((uint32_t)(v + 1)) - 1; }  // v >= -1
+
+// With a window, a bound from below on the first shared key that a served row sees of
+// those that a block of this lane's row can have: of its group, and at most TB / G of them.
+// The lanes have the rows first .. first + 63.
+__device__ inline int block_first(const SharedArgs& x, const SharedRow& s, int first) {
+  const int lane = own_tid() % WAVE;  // (the lanes' addresses would be kept, too)
+  int low = s.row.p0 < 0 ? FAR : s.row.p0;
+#pragma unroll
+  for (int off = 1; off < WAVE; off *= 2) {
+    const int from = min(lane + off, WAVE - 1) * 4;  // the last lane's own rows are in all of them
+    const int v = __builtin_amdgcn_ds_bpermute(from, low);
+    if (__builtin_amdgcn_ds_bpermute(from, s.name) == s.name) low = min(low, v);
+  }
+  if (first + WAVE < x.n) {  // a group that goes on behind the lanes
+    const int name = load_scalar(x.lead, first + WAVE);
+    int behind = FAR;
+    for (int i = first + WAVE; i < min(x.n, first + WAVE + TB / x.a.G - 1); i += WAVE) {
+      const int b = min(i + lane, x.n - 1), p0 = lane_row(x.a.b, b, nullptr).p0;
+      if (x.lead[b] == name && p0 >= 0) behind = min(behind, p0);
+    }
+    behind = FAR - lane_max(FAR - behind);
+    if (s.name == name) low = min(low, behind);
+  }
+  return max(0, low - x.a.window + 1);
+}
 
 template <class T, int DP, bool FULL, bool E8>
 __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(SharedArgs x) {
@@ -162,7 +187,7 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
   // of the rows i0 .. i0 + 63 (each wave finds the same): what would stand in the
   // way of the tiles' registers
   __shared__ struct {
-    int steps[WAVE], up_at[WAVE], lead[WAVE], name[WAVE], prefix[WAVE], lead_seq[WAVE], kind[WAVE];
+    int steps[WAVE], skip[WAVE], up_at[WAVE], lead[WAVE], name[WAVE], prefix[WAVE], lead_seq[WAVE], kind[WAVE];
     int groups[WAVE], us_at[WAVE], p0[WAVE], seq[WAVE];
   } rows;
   RowsLds& rl = *(RowsLds*)lds;
@@ -175,15 +200,25 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
   int32_t* const err = blockIdx.x == 0 && threadIdx.x < WAVE ? a.err : nullptr;
 
   // A lane's row, its blocks' weight on the line (up: its tile of all heads, us:
-  // its own keys), and the weights up to it.
+  // its own keys), and the weights up to it; steps: units of the shared keys, behind
+  // `skip` of them that no row sees.
   SharedRow sr;
-  int steps, groups, up, us, up_at, us_at;
+  int steps, skip, groups, up, us, up_at, us_at;
   auto load = [&](int first, int run_before, int32_t* e) {
+    const int lane = own_tid() % WAVE;
     sr = shared_row<TILES>(x, first, run_before, e);
     const bool here = first + lane < n;
     steps = sr.lead >= 0 && here && (first + lane - sr.lead) % (kind_rows(sr.kind) / a.G) == 0
                 ? div_up_pos(sr.prefix, sr.kind == TILE ? TC::KB : GROUP)
                 : 0;
+    // shared keys before the windows of all its rows cost nothing (one unit stays, for the
+    // join, where all are)
+    skip = 0;
+    if (a.window) {
+      const int units = block_first(x, sr, first) / (sr.kind == TILE ? TC::KB : GROUP);
+      skip = max(0, min(units, steps - 1));
+      steps -= skip;
+    }
     groups = own_groups<KS>(sr.row.p0, sr.prefix, a.window);
     up = steps ? x.cost(sr.kind == TILE).block(steps) * a.Hkv : 0;
     us = here ? x.cost_own(groups).block(groups) * nb : 0;
@@ -253,8 +288,9 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
       minpos = uniform(maxpos < 0 ? 0 : FAR - lane_max(FAR - minpos));
       nrow = uniform(cnt) * a.G;
       const int keys = tile ? TC::KB : GROUP;
-      kbeg = max(a.window && maxpos >= 0 ? minpos - a.window + 1 : 0, c0 * keys);
-      kend = min(min(p, maxpos + 1), c1 * keys);
+      const int skip = uniform(rows.skip[at]);
+      kbeg = max(a.window && maxpos >= 0 ? minpos - a.window + 1 : 0, (skip + c0) * keys);
+      kend = min(min(p, maxpos + 1), (skip + c1) * keys);
       if (kbeg >= kend) kbeg = kend = 0;
       if constexpr (TILES) {
         if (tile) {
@@ -378,6 +414,7 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
     }
     if (wave == 0) {
       rows.steps[lane] = steps;
+      rows.skip[lane] = skip;
       rows.up_at[lane] = pb + up_at - up;
       rows.lead[lane] = sr.lead;
       rows.name[lane] = sr.name;
@@ -565,18 +602,22 @@ hipError_t launch_attn_shared(const np_kv_shape& s, int layer, const np_kv_batch
       n * s.kv_heads *
           ((std::min<int64_t>(sh.max_prefix, x.a.b.lim) / 32 + 1) * x.tile.w + x.tile.fix + x.own.fix) +
       heads * (((int64_t)x.a.b.lim / GROUP + 2) * x.own.w + x.own.fix);
-  // What sharing saves is at most the prefix's bytes for all rows but one; the join,
-  // and the search for the groups, cost 4 us and 0.1 a row, about what 32 MB and 1
-  // MB a row take to read.  Us apart / shared (bf16, 32 heads over 8 of 128; the
+  // What sharing saves is at most the bytes of the prefix, or of a window of it, for all
+  // rows but one; the join, and the search for the groups, cost 4 us and 0.1 a row, about
+  // what 32 MB and 1 MB a row take to read.  Us apart / shared (bf16, 32 heads over 8 of 128; the
   // bytes in brackets): 2 rows behind 2048 keys 11 / 15 (8 MB), behind 8192 22 / 20 (34
   // MB); 8 rows behind 512 9 / 15 (15 MB), behind 2048 18 / 16 (59 MB); 32 rows behind
-  // 512 18 / 20 (65 MB), behind 2048 33 / 23 (260 MB).
-  const int64_t saved = (n - 1) * sh.max_prefix * s.kv_heads * 2 * kv_row_bytes(s);
+  // 512 18 / 20 (65 MB), behind 2048 33 / 23 (260 MB).  With a window half as much again (48
+  // rows of 64 over 8 behind 32768, windows of 600, 1000 and 4096 keys: 21.5 / 26.8, 28.8 /
+  // 28.3, 102 / 37; 8 of 32 over 8 of 256, 1000 and 4096: 19.8 / 24.6, 53 / 39; where keys
+  // that no row sees stood on the line too, 256 to 4096 took 64 to 69 us of the first).
+  const int64_t seen = window > 0 ? std::min(sh.max_prefix, window) : sh.max_prefix;
+  const int64_t saved = (n - 1) * seen * s.kv_heads * 2 * kv_row_bytes(s);
   // Rows of up to 256 keys of 8-bit elements, many blocks: np_attn_decode has a wave for each
   // (36 rows of 40 heads over 40, 192 keys shared, 17.3 / 20.1; 160 of 32 over 32 34.2 / 37.5
   // to 41.3; plain fp16 25.0 / 21.9, 50.0 / 47.9).
   const bool brief = kv_e4m3(s) && x.a.b.lim <= 256 && (int64_t)x.a.tiles * s.kv_heads > 768;
-  if (saved < (32 + n) * 1000000 || brief || line >= ((int64_t)1 << 30)) return apart();
+  if (saved < (32 + n) * (window > 0 ? 1500000 : 1000000) || brief || line >= ((int64_t)1 << 30)) return apart();
   KvScratch k;
   kv_ws_layout(s, (char*)ws, &k);
   x.lead = sh.lead;

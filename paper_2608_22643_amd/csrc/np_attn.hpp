@@ -1475,6 +1475,35 @@ hipError_t launch_tile(AttnArgs a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// Whether even shares deal more than 768 blocks of up to 256 keys better than a wave for
+// each block does.  The card has 1024 such blocks at once, a workgroup of four on every
+// compute unit; units that get one more take up to twice as long over long blocks, while
+// the shares stay even.  Us, even shares / a wave each, 32 heads over 32, rows of 1 to `keys`
+// keys, by the number of blocks:
+//                       1024         1088         1280         1536         1792         2176
+//   fp32 128, 256  39.9 / 39.6  42.6 / 63.2  51.5 / 65.2  59.6 / 66.2  62.9 / 69.0  73.8 / 89.4
+//        128, 128  20.6 / 18.1  28.4 / 30.1  30.2 / 34.6  30.9 / 34.7  40.0 / 35.8  48.7 / 40.6
+//         64, 256  24.6 / 21.4  24.8 / 29.3  31.5 / 33.2  35.5 / 34.9  37.7 / 36.3  42.7 / 47.4
+//         64, 128  13.4 / 11.2  17.4 / 15.4  17.8 / 16.8  18.0 / 17.0  23.0 / 18.0  28.1 / 20.5
+//        256, 256  79.8 / 70.5  82.9 / 83.1   103 / 101    117 / 105    122 / 119    144 / 128
+//   fp16 128, 256  24.2 / 20.2  25.9 / 30.5  31.6 / 31.6  35.5 / 32.7  37.6 / 34.8  43.3 / 42.1
+//        128, 128  12.4 / 10.0  15.4 / 13.3  16.1 / 15.1  16.6 / 15.1  20.7 / 16.6  25.9 / 19.1
+//   fp32 and 8-bit elements:
+//        128, 256  34.8 / 28.9  34.4 / 43.3  35.8 / 46.5  42.7 / 46.7  43.1 / 47.2  52.3 / 54.7
+//        128, 128  22.0 / 16.8  21.9 / 22.7  22.1 / 25.6  22.3 / 25.5  33.4 / 25.8  33.8 / 26.0
+// Rows that all have 256 keys: fp32 of 256, 1088 blocks, 112 / 138.  16-bit heads over 8-bit
+// elements of up to 128 take 0.34 to 1.09 of the even shares' time throughout.
+template <class T, int DP, bool E8>
+bool shares_better(int D, int64_t blocks, int64_t keys) {
+  const int64_t rounds = (blocks + 1023) / 1024, bytes = keys * D * (16 / T::V);
+  auto filled_below = [&](int percent) { return blocks * 100 < rounds * 1024 * percent; };
+  if (E8) return T::V == 4 && keys > 64 && rounds == 2 && filled_below(80);
+  if (DP == 256) return bytes > 192 * 1024 && rounds == 2 && filled_below(65);
+  if (T::V == 8) return bytes > 48 * 1024 && rounds == 2 && filled_below(65);
+  return (bytes > 48 * 1024 && rounds == 2 && filled_below(80)) ||
+         (keys > 192 && D == DP && (rounds == 2 || rounds == 3) && filled_below(90));
+}
+
 // keys: the most a block can see.  Four ways to deal the keys of `blocks`
 // blocks to workgroups (us, fp16 or bf16, D 128, before -> with the rule):
 //  - Every 128 keys to a workgroup of its own while all of them fit on the card
@@ -1496,7 +1525,7 @@ hipError_t launch_tile(AttnArgs a, hipStream_t stream) {
 //    heads over 32 11.1 / 6.1, 19.7 / 12.9, 22.2 / 21.3, 160 rows 30.8 / 13.5, 53.6 /
 //    36.5, 96.6 / 72.4; fp16 36.4 / 18.9, 87.8 / 75.0, 152 / 145; fp32 of 64 and 8-bit
 //    elements 34.3 / 17.2, 71 / 47, 109 / 95; but with 512 blocks, 64 rows of 32 over
-//    8, of 256 keys 12.6 / 11.6, 13.3 / 13.8, 14.6 / 19.6.
+//    8, of 256 keys 12.6 / 11.6, 13.3 / 13.8, 14.6 / 19.6.  But see shares_better.
 // Prompts (rows of more tokens) have many blocks; they are split while those do
 // not give every compute unit two workgroups (64 tokens of 32 heads over 8 behind
 // 2000 others: 29 with one a compute unit, 23 with two), or one if they are few
@@ -1516,7 +1545,7 @@ hipError_t launch_rows(AttnArgs a, int64_t keys, int max_tokens, hipStream_t str
     hipLaunchKernelGGL(kernel, grid, dim3(ROWS_T), 0, stream, a);
     return hipGetLastError();
   };
-  if (!a.b.cu && !small && blocks > 768 && keys <= 256) {
+  if (!a.b.cu && !small && blocks > 768 && keys <= 256 && !shares_better<T, DP, E8>(a.D, blocks, keys)) {
     grid = block_grid((blocks + NWAVE - 1) / NWAVE);
     if (a.D == DP) return go(attn_waves_kernel<T, DP, true, E8>);
     return go(attn_waves_kernel<T, DP, false, E8>);

@@ -424,9 +424,10 @@ def make_kv_shape(layers, heads, kv_heads, head_dim, page_size, n_pages, max_seq
                        DTYPE_CODE.get(dtype, dtype) | CACHE_CODE[cache])
 
 
-def _elem_size(dtype: int) -> int:
-    """Bytes of an element of the heads of np_kv_shape.dtype."""
-    return 4 if dtype & ~NP_KV_E4M3 == NP_F32 else 2
+def _of_heads_type(x, shape: np_kv_shape) -> bool:
+    """Whether tensor x has the type of the heads of np_kv_shape."""
+    names = {NP_F32: "torch.float32", NP_F16: "torch.float16", NP_BF16: "torch.bfloat16"}
+    return str(x.dtype) == names.get(shape.dtype & ~NP_KV_E4M3)
 
 
 def kv_pool_shape(shape: np_kv_shape) -> tuple[int, ...]:
@@ -530,7 +531,7 @@ def np_kv_append_norm(shape, layer: int, batch: np_kv_batch, page_table, rows: n
                       rotary, pool, ws, stream=None) -> None:
     for w in getattr(norm, "_kept", ()):
         if w is not None and (w.numel() != shape.head_dim
-                              or w.element_size() != _elem_size(shape.dtype)):
+                              or not _of_heads_type(w, shape)):
             raise ValueError(f"weights: {shape.head_dim} values of the heads' type")
     _check(lib().np_kv_append_norm(ctypes.byref(shape), int(layer), ctypes.byref(batch),
                                    _p(page_table), ctypes.byref(rows),
@@ -545,7 +546,7 @@ def np_kv_read(shape, layer: int, batch: np_kv_batch, page_table, pool, k_out, v
     for x in (k_out, v_out):
         if x is not None and (tuple(x.shape[1:]) != (shape.kv_heads, shape.head_dim)
                               or x.shape[0] < batch.n_tokens
-                              or x.element_size() != _elem_size(shape.dtype)):
+                              or not _of_heads_type(x, shape)):
             raise ValueError(f"k_out and v_out: [{batch.n_tokens}][{shape.kv_heads}]"
                              f"[{shape.head_dim}] tensors of the heads' type")
     ks, vs = (0 if x is None else _token_stride(x) for x in (k_out, v_out))

@@ -285,6 +285,22 @@ class DecoderLayers:
         return x
 
 
+def check_samples(net: DecoderLayers, x, prompt: int, total: int) -> None:
+    """x [samples][d_model] of samples that had the same `total` tokens, `prompt` of them shared.  Bit for bit the same
+    where np_attn_decode cuts their keys alike: up to 768 groups of 128 keys, and less than 32 MB that sharing the prompt
+    could save.  Beyond that their attention may differ by roundings, which the layers pass on."""
+    n, dt = x.shape[0], net.cfg.adtype
+    groups = n * net.kv_heads * -(-net.heads // net.kv_heads // 16) * -(-total // 128)
+    row = net.head_dim * (1 if net.cache.pool.dtype == torch.uint8 else x.element_size())
+    if groups <= 768 and (n - 1) * prompt * net.kv_heads * 2 * row < 32_000_000:
+        assert all(torch.equal(x[0], x[i]) for i in range(n)), "samples of the same tokens agree"
+        return
+    off = (x.float() - x[:1].float()).abs().max() / x.float().abs().max()
+    # (a key or value that falls to the other side of a border of 8-bit elements is off by a sixteenth)
+    most = 0.05 if net.cache.pool.dtype == torch.uint8 else {"f32": 1e-4, "f16": 0.02, "bf16": 0.05}[dt]
+    assert off <= most, f"samples of the same tokens agree: off by {float(off):.2g} of the largest output"
+
+
 def main(argv=None) -> None:
     import argparse
     import time
@@ -308,7 +324,8 @@ def main(argv=None) -> None:
     prompt_out = net.step(h[:args.prompt], cache.extend([0], [args.prompt], args.prompt))
     cache.fork([0] * n, range(1, n + 1))
     pages = cache.pages_used()
-    shared = cache.share([0] * n, [args.prompt] * n)  # the prompt is read once for all samples
+    # the prompt is read once for all samples, where that is worth a second kernel
+    shared = cache.share([0] * n, [args.prompt] * n)
     torch.cuda.synchronize()
     t0 = time.perf_counter()
     for t in range(args.prompt, total):
@@ -316,9 +333,7 @@ def main(argv=None) -> None:
     torch.cuda.synchronize()
     dt = time.perf_counter() - t0
     assert torch.isfinite(prompt_out.float()).all() and torch.isfinite(x.float()).all()
-    # (not bit for bit: their sums over a shared prefix may be cut at other keys)
-    off = (x.float() - x[:1].float()).abs().max() / x.float().abs().max()
-    assert off <= 0.05, "samples of the same tokens agree"
+    check_samples(net, x, args.prompt, total)
     used = cache.pages_used()
     cache.free([0])
     cache.compact()

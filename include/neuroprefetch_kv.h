@@ -299,7 +299,10 @@ np_status np_attn_prompt(const np_kv_shape* shape, int32_t layer, const np_kv_ba
  * some 30 MB of keys and values it is not worth the second kernel, nor for many short
  * rows of 8-bit elements), and for batches
  * of more than 32768 query heads in all, or more than 128 query heads per key-value
- * head (16 in fp32), it is np_attn_decode, leads and prefixes then unread. */
+ * head (16 in fp32), it is np_attn_decode, leads and prefixes then unread.  A value of
+ * a group's prefix that is not finite, at a position that some row of the group sees,
+ * may also reach rows of the group that do not see it (their window has passed it, or
+ * they end before it); rows of other groups it does not. */
 np_status np_attn_decode_shared(const np_kv_shape* shape, int32_t layer, const np_kv_batch* batch,
                                 const np_kv_shared* shared, const int32_t* page_table,
                                 const void* q, int64_t q_stride, const void* pool, float scale,

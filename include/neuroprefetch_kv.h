@@ -168,8 +168,8 @@ typedef struct np_qk_norm {
  * them, which names itself.  Sequence seqs[b] then has the same keys and values
  * at positions 0 .. prefix[lead[b]] - 1 as sequence seqs[lead[b]] (as np_kv_fork
  * makes them: the same pages, and copies of a partly filled last one); those of
- * the latter are read.  prefix of other rows is not read.  max_prefix: a host
- * value that no group's prefix exceeds.  A lead outside [0, b], one that does not
+ * the latter are read.  prefix of other rows is not read; of a prefix past max_len the
+ * positions below it count.  max_prefix: a host value that no group's prefix exceeds.  A lead outside [0, b], one that does not
  * name itself, whose rows do not lie next to each other, whose sequence is outside
  * [0, S), or whose prefix is outside [0, max_prefix] sets NP_DEVERR_STATE, and the
  * row is computed by itself, from its own pages, as in np_attn_decode. */
@@ -248,8 +248,8 @@ np_status np_kv_append(const np_kv_shape* shape, int32_t layer, const np_kv_batc
                        const np_rotary* rotary, void* pool, void* dev_ws, hipStream_t stream);
 
 /* The same behind a norm of each query and key head (norm NULL: none), all in
- * 32 bits up to the one rounding to w (keys of 8-bit caches in 64).  q_out,
- * strides and what is not served as above.  One kernel. */
+ * 32 bits up to the one rounding to w (keys of 8-bit caches in 64, rounded to 32 before
+ * it).  q_out, strides and what is not served as above.  One kernel. */
 np_status np_kv_append_norm(const np_kv_shape* shape, int32_t layer, const np_kv_batch* batch,
                             const int32_t* page_table, const np_kv_rows* rows,
                             const np_qk_norm* norm, const np_rotary* rotary, void* pool,

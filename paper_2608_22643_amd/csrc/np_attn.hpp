@@ -250,8 +250,8 @@ __device__ inline float sum_groups(float v) {
 // 777 keys and 32 heads.  fp32 prompts run here too: 4096 tokens of 16 heads over
 // 4 at 81, 74 and 93 TFLOP/s for heads of 64, 128 and 256 (an 8192^3 fp32 library
 // product reaches 149 to 154).  8-bit elements become w on their way to the matrix
-// cores: one row of 131071 keys, 8 key-value heads of 128, 270 MB in 47 us (5.7 TB/s);
-// 777 keys and 32 heads 8.8 us.
+// cores: one row of 131071 keys, 8 key-value heads of 128, 270 MB in 47 to 56 us (4.8 to 5.7
+// TB/s, from card to card); 777 keys and 32 heads 8.8 us.
 // ---------------------------------------------------------------------------
 constexpr int RB = 16;
 constexpr int NWAVE = 4;
@@ -976,9 +976,9 @@ __global__ __launch_bounds__(ROWS_T, DP < 256 ? (E8 ? 3 : 2) : E8 ? 2 : 1) void 
 // 2048 fp16 tokens and 32 heads 62 to 65 us (530 to 550 TFLOP/s; a library product
 // of as many operations 52 to 57 us).
 // 8-bit elements become w between registers and LDS; the second product reads as
-// before, at the same rates (8192 bf16 tokens of 64 heads over 8 of 128: 1.12 ms, 984
-// TFLOP/s).  Two stores a row meet in half of the banks; in an order of theirs that
-// does not it takes as long.
+// before, at the same rates from heads of 80 on (8192 bf16 tokens of 64 heads over 8 of 128:
+// 1.12 ms, 984 TFLOP/s; 4096 of 32 over 8 of 64: 119 us, of 16-bit elements 98).  Two stores
+// a row meet in half of the banks; in an order of theirs that does not it takes as long.
 // Measured and dropped: one workgroup of eight waves in two groups half a step
 // apart, 4.68 to 5.05 ms; the next step's score products dealt between this step's
 // exponentials, 4.56 ms (16384 tokens) and 119 against 106 us (packed prompts).
@@ -1545,7 +1545,8 @@ hipError_t launch_rows(AttnArgs a, int64_t keys, int max_tokens, hipStream_t str
     hipLaunchKernelGGL(kernel, grid, dim3(ROWS_T), 0, stream, a);
     return hipGetLastError();
   };
-  if (!a.b.cu && !small && blocks > 768 && keys <= 256 && !shares_better<T, DP, E8>(a.D, blocks, keys)) {
+  if (!a.b.cu && !small && blocks > 768 && keys <= 256 &&
+      !shares_better<T, DP, E8>(a.D, blocks, keys)) {
     grid = block_grid((blocks + NWAVE - 1) / NWAVE);
     if (a.D == DP) return go(attn_waves_kernel<T, DP, true, E8>);
     return go(attn_waves_kernel<T, DP, false, E8>);

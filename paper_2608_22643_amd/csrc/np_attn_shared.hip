@@ -12,7 +12,7 @@
 // What it costs beside the keys: the groups' search (2 us), a first step (5 to 7) and
 // the join (4 to 9).  32 fp16 rows of 32 heads over 8 of 128 in four groups behind up to 3000
 // keys take 22 us (np_attn_decode 35, of which the reads are 6.5): latencies in line.  48 bf16 rows
-// of 64 heads over 8 behind 32768 keys of 8-bit elements take 80 to 87 us (np_attn_decode 430,
+// of 64 heads over 8 behind 32768 keys of 8-bit elements take 80 to 91 us (np_attn_decode 430,
 // the products alone 37 at the rate of a large one): 27 steps of a tile in each workgroup at
 // 2.2 to 2.9 us, and 33 MB of parts written and read.
 //
@@ -187,8 +187,8 @@ __global__ __launch_bounds__(ROWS_T, DP == 256 ? 1 : 2) void attn_shared_kernel(
   // of the rows i0 .. i0 + 63 (each wave finds the same): what would stand in the
   // way of the tiles' registers
   __shared__ struct {
-    int steps[WAVE], skip[WAVE], up_at[WAVE], lead[WAVE], name[WAVE], prefix[WAVE], lead_seq[WAVE], kind[WAVE];
-    int groups[WAVE], us_at[WAVE], p0[WAVE], seq[WAVE];
+    int steps[WAVE], skip[WAVE], up_at[WAVE], lead[WAVE], name[WAVE], prefix[WAVE], lead_seq[WAVE];
+    int kind[WAVE], groups[WAVE], us_at[WAVE], p0[WAVE], seq[WAVE];
   } rows;
   RowsLds& rl = *(RowsLds*)lds;
 
@@ -598,16 +598,18 @@ hipError_t launch_attn_shared(const np_kv_shape& s, int layer, const np_kv_batch
   x.least = 4;
   x.small = dtype == NP_F32 ? 0 : 32;
   // the line's length: at most a block of shared keys a row, and every row's own
+  const int64_t longest = std::min<int64_t>(sh.max_prefix, x.a.b.lim);
   const int64_t line =
-      n * s.kv_heads *
-          ((std::min<int64_t>(sh.max_prefix, x.a.b.lim) / 32 + 1) * x.tile.w + x.tile.fix + x.own.fix) +
+      n * s.kv_heads * ((longest / 32 + 1) * x.tile.w + x.tile.fix + x.own.fix) +
       heads * (((int64_t)x.a.b.lim / GROUP + 2) * x.own.w + x.own.fix);
   // What sharing saves is at most the bytes of the prefix, or of a window of it, for all
   // rows but one; the join, and the search for the groups, cost 4 us and 0.1 a row, about
   // what 32 MB and 1 MB a row take to read.  Us apart / shared (bf16, 32 heads over 8 of 128; the
   // bytes in brackets): 2 rows behind 2048 keys 11 / 15 (8 MB), behind 8192 22 / 20 (34
   // MB); 8 rows behind 512 9 / 15 (15 MB), behind 2048 18 / 16 (59 MB); 32 rows behind
-  // 512 18 / 20 (65 MB), behind 2048 33 / 23 (260 MB).  With a window half as much again (48
+  // 512 18 / 20 (65 MB), behind 2048 33 / 23 (260 MB); what the groups really save only the
+  // device knows: 32 rows behind 2048 as four groups 35 / 26, as pairs 44 / 35, alone 48 / 51;
+  // of 64 over 8 behind 4096 in 8-bit elements 39 / 29, 41 / 45, 48 / 52.  With a window half as much again (48
   // rows of 64 over 8 behind 32768, windows of 600, 1000 and 4096 keys: 21.5 / 26.8, 28.8 /
   // 28.3, 102 / 37; 8 of 32 over 8 of 256, 1000 and 4096: 19.8 / 24.6, 53 / 39; where keys
   // that no row sees stood on the line too, 256 to 4096 took 64 to 69 us of the first).
@@ -617,7 +619,8 @@ hipError_t launch_attn_shared(const np_kv_shape& s, int layer, const np_kv_batch
   // (36 rows of 40 heads over 40, 192 keys shared, 17.3 / 20.1; 160 of 32 over 32 34.2 / 37.5
   // to 41.3; plain fp16 25.0 / 21.9, 50.0 / 47.9).
   const bool brief = kv_e4m3(s) && x.a.b.lim <= 256 && (int64_t)x.a.tiles * s.kv_heads > 768;
-  if (saved < (32 + n) * (window > 0 ? 1500000 : 1000000) || brief || line >= ((int64_t)1 << 30)) return apart();
+  const int64_t asked = (32 + n) * (window > 0 ? 1500000 : 1000000);
+  if (saved < asked || brief || line >= ((int64_t)1 << 30)) return apart();
   KvScratch k;
   kv_ws_layout(s, (char*)ws, &k);
   x.lead = sh.lead;

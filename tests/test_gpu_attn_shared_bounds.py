@@ -16,8 +16,6 @@ MOST = 2 ** 31 - 1
 def test_prefixes_past_all_positions(dtype, cache, Hq, Hkv, D, prefix):
     """Rows that all end inside a prefix of up to 2^31 - 1 positions see their own keys of it; a group with a true
     prefix beside them."""
-    if dtype == "f32" and Hq // Hkv > 16:
-        pytest.skip("more than 16 query heads a key-value head: np_attn_decode")
     s = Setup([(300, [0, -5, -100, -299]), (70, [2, 9])], Hq, Hkv, D, 16, dtype, cache, seed=30)
     out = s.run(s.shared(prefix=[prefix, 0, 0, 0, 70, 0], most=MOST))
     s.check(out)
